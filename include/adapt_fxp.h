@@ -102,6 +102,8 @@ int adapt_set_stream(adapt_ctx *ctx, void *hip_stream);
  *   KLD_SEARCH                             n, wl_lo, wl_hi, bins
  *   KLD_SEARCH_BATCHED                     kld_items (HOST array; only n and bins are read), count, wl_lo, wl_hi
  *   GRADIENT_DIVERSITY                     n, count
+ *   LOG_PROBS                              n = rows, K = classes, count = topk, fa = format of the logits
+ *   CROSS_ENTROPY                          n = rows, K = classes, fa = format of the logits, fb = of the gradient
  * Returns the workspace_bytes with which the call takes its preferred plan (all K splits, padded
  * copies of narrow layers, one batch for up to 24 searches) and returns neither ADAPT_EWORKSPACE nor
  * ADAPT_EBOUND; 0 for a query that is invalid.  With less, contractions use fewer K splits and
@@ -112,7 +114,7 @@ typedef enum {
     ADAPT_CALL_QUANTIZE = 0, ADAPT_CALL_QUANTIZE_BATCHED = 1, ADAPT_CALL_GEMM = 2, ADAPT_CALL_CONV_FWD = 3,
     ADAPT_CALL_CONV_DGRAD = 4, ADAPT_CALL_CONV_WGRAD = 5, ADAPT_CALL_CONV_BACKWARD = 6, ADAPT_CALL_KLD_SEARCH = 7,
     ADAPT_CALL_KLD_SEARCH_BATCHED = 8, ADAPT_CALL_SGD_UPDATE = 9, ADAPT_CALL_GRADIENT_DIVERSITY = 10,
-    ADAPT_CALL_REQUANTIZE_FIT = 11
+    ADAPT_CALL_REQUANTIZE_FIT = 11, ADAPT_CALL_LOG_PROBS = 12, ADAPT_CALL_CROSS_ENTROPY = 13
 } adapt_call;
 struct adapt_kld_item_s;
 typedef struct {
@@ -499,6 +501,68 @@ int adapt_gap_bwd(adapt_ctx *ctx, const void *dout, int wl, int n, int hw, int c
 int adapt_grad_add(adapt_ctx *ctx, const void *a, int wl_a, const int64_t *e_a, const void *b,
                    int wl_b, const int64_t *e_b, size_t n, int wl_out, adapt_rng rng, void *out,
                    int32_t *shift, int64_t *e_out);
+
+/* ---- dropout, log probabilities and softmax cross entropy on fixed-point codes -----------------
+ * What a network needs between its layers and behind the last one.  The paper's networks are trained
+ * with dropout and a softmax loss (Sec. 4.1) and it does not say how either is carried out on codes;
+ * the rules below are this library's.  Pointers of these three calls need the alignment of their
+ * elements only; the context's device has to be the current one (ADAPT_EINVAL otherwise). */
+
+/* Dropout of n codes with drop probability p, scaled so that the expectation stays.  No mask is
+ * stored: R = the 16 random bits of element i from rng's seed and stream (whatever its mode).  With
+ * T = floor(p 2^16 + 1/2), K = 2^16 - T, s = fo.fl - fx.fl, X = floor(x 2^(16+s)):
+ *   y   = floor((X + u)/K) if R >= T, else 0;   u = R - T (SR), floor(K/2) (RN_HALF_UP)
+ *   out = y + res 2^(fo.fl - fres.fl), saturated to fo.wl bits
+ * One draw decides both whether the element stays and how it is rounded: given R >= T, u is uniform
+ * on 0..K-1, so that y is rounded up with probability (X mod K)/K and its expectation over the
+ * draws is exactly X 2^-16.
+ * The gradient is the same call on the gradient's codes, with the same p, seed and stream.
+ *   x    device, n codes of format fx (wl up to 32);  out  device, n codes of format fo; may be x or res
+ *        where that has codes of the same size
+ *   res  device, n codes of format fres that are added, or NULL (fres is then ignored)
+ * 0 <= p, T <= 65535; n <= 2^40.  ADAPT_EUNSUPPORTED: fo.fl - fx.fl > 15, or fres.fl > fo.fl (the
+ * residual is added as it is, not rounded). */
+int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t n, double p, adapt_fmt fo,
+                  adapt_rng rng, const void *res, adapt_fmt fres, void *out);
+
+/* The logits of the two calls below: `rows` rows of `classes` values, row i at logits + i*ld
+ * (ld >= classes, in elements), as codes of format f, or as fp32 where f.wl == ADAPT_WL_FP32 (f.fl is
+ * then ignored).  With x_ij the value of logit j of row i and labels device int64_t[rows]:
+ *   lse_i = log sum_j exp(x_ij),  p_ij = exp(x_ij - lse_i)   (natural logarithm)
+ *   labels[i] in 0..classes-1 names a class; a negative one says that the row has none; one of
+ *   classes or more is an error of the caller's that gives NaN as the row's logp (and a gradient of 0).
+ * fp32 logits may be -inf (a masked class: p = 0).  A row of nothing but -inf has lse = -inf, entropy
+ * 0, a logp of -inf for every class and a gradient of 0.  A NaN or +inf makes lse, entropy and the
+ * logps of its row NaN and the row's gradient 0.
+ * 1 <= classes <= 2^30, rows < 2^31, rows * ld <= 2^40.  rows = 0 is valid. */
+#define ADAPT_WL_FP32 0
+
+/* Log probabilities of given classes, and the largest ones.
+ *   logp     device float[rows] or NULL: x_i,label - lse_i; 0 for a row without label.  labels may
+ *            be NULL if logp is
+ *   lse      device float[rows] or NULL;  entropy  device float[rows] or NULL: -sum_j p_ij log p_ij
+ *   topk     0..32, at most classes: top_index = device int32_t[rows*topk], the classes of the topk
+ *            largest logits of each row, largest first, equal ones (and +0, -0) by their index; a NaN
+ *            counts as -inf.  top_logp = device float[rows*topk], their log probabilities.  Both may
+ *            be NULL if topk is 0
+ * Workspace: adapt_workspace_bytes with ADAPT_CALL_LOG_PROBS. */
+int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes,
+                    size_t ld, const int64_t *labels, float *logp, float *lse, float *entropy,
+                    int topk, int32_t *top_index, float *top_logp);
+
+/* Softmax cross entropy and its gradient as the codes that adapt_net_backward takes:
+ *   logp      device float[rows] or NULL, as above (the loss of the batch is -sum_i weights_i logp_i)
+ *   dlogits   device codes of format fg (wl up to 32), row i at dlogits + i*ldg (ldg >= classes):
+ *             quantize(weights_i (p_ij - [j = labels_i])) by adapt_quantize's rule for the real
+ *             value (evaluated in 64 bits), with the random bits of element i*classes + j.
+ *             0 in rows without label.  Must not overlap the logits
+ *   weights   device float[rows], or NULL for 1 everywhere (a mean over the rows is a power of two in
+ *             fg.fl and a weight)
+ * |p - [..]| <= 1, so fg.fl = fg.wl - 1 loses nothing but the code of exactly 1.
+ * Workspace: adapt_workspace_bytes with ADAPT_CALL_CROSS_ENTROPY. */
+int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes,
+                        size_t ld, const int64_t *labels, const float *weights, adapt_fmt fg,
+                        adapt_rng rng, void *dlogits, size_t ldg, float *logp);
 
 /* A feed-forward chain of convolution / fully connected layers (FC: h = w = r = s = 1, pad 0, c =
  * the flattened NHWC input), each optionally followed by ReLU (fused into the contraction's

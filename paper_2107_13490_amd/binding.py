@@ -76,7 +76,8 @@ class WorkspaceQuery(C.Structure):
 
 
 (CALL_QUANTIZE, CALL_QUANTIZE_BATCHED, CALL_GEMM, CALL_CONV_FWD, CALL_CONV_DGRAD, CALL_CONV_WGRAD, CALL_CONV_BACKWARD,
- CALL_KLD_SEARCH, CALL_KLD_SEARCH_BATCHED, CALL_SGD_UPDATE, CALL_GRADIENT_DIVERSITY, CALL_REQUANTIZE_FIT) = range(12)
+ CALL_KLD_SEARCH, CALL_KLD_SEARCH_BATCHED, CALL_SGD_UPDATE, CALL_GRADIENT_DIVERSITY, CALL_REQUANTIZE_FIT, CALL_LOG_PROBS,
+ CALL_CROSS_ENTROPY) = range(14)
 
 
 class GradItem(C.Structure):
@@ -192,6 +193,9 @@ def load_library():
     lib.adapt_gap_fwd.argtypes = [vp, vp, Fmt, i, i, i, Rng, vp]
     lib.adapt_gap_bwd.argtypes = [vp, vp, i, i, i, i, vp]
     lib.adapt_grad_add.argtypes = [vp, vp, i, vp, vp, i, vp, sz, i, Rng, vp, vp, vp]
+    lib.adapt_dropout.argtypes = [vp, vp, Fmt, sz, dbl, Fmt, Rng, vp, Fmt, vp]
+    lib.adapt_log_probs.argtypes = [vp, vp, Fmt, sz, sz, sz, vp, vp, vp, vp, i, vp, vp]
+    lib.adapt_cross_entropy.argtypes = [vp, vp, Fmt, sz, sz, sz, vp, vp, Fmt, Rng, vp, sz, vp]
     lib.adapt_net_workspace_bytes.argtypes = [C.POINTER(LayerDesc), i, i]
     lib.adapt_net_workspace_bytes.restype = sz
     lib.adapt_net_create.argtypes = [vp, C.POINTER(LayerDesc), i, C.POINTER(vp), C.POINTER(SwitchParams), vp, sz, C.POINTER(vp)]
@@ -296,6 +300,18 @@ def _fmt(f):
     return r
 
 
+_FP32 = Fmt(0, 0)      # fp32 logits
+
+
+def _dense_rows(t):
+    """A matrix whose rows are dense and do not overlap."""
+    return t.numel() == 0 or ((t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]))
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 and t.shape[1] > 0 else t.shape[1]
+
+
 # Descriptor arrays of the batched calls: the values of all items in order, packed at once.  Building one ctypes structure per item
 # costs more host time than the call (a window of 25 gradients 17 us, packed 7).  What does not pack (a negative stream, a word
 # length that is no integer or longer than its field) goes into the structures, which wrap or refuse it.
@@ -323,6 +339,7 @@ class Context:
             raise RuntimeError("paper_2107_13490_amd needs a HIP device; there is no CPU path")
         self._lib = load_library()
         self._torch = torch
+        self._device = torch.cuda.current_device()
         s = stream if stream is not None else torch.cuda.current_stream()
         self._stream = s
         h = C.c_void_p()
@@ -712,6 +729,85 @@ class Context:
                                         a.numel(), wl_out, Rng(mode, seed, stream), _ptr(out), _ptr(shift), _ptr(e_out)),
                "adapt_grad_add")
         return out, shift, e_out
+
+    # -- dropout, log probabilities, cross entropy --------------------------------------------------
+    def _own(self, what, t, shape=None, dtype=None, rows=False):
+        """Checks a tensor of the calls below: on the context's device, of the given shape and type, dense (rows: with
+        dense rows)."""
+        if not t.is_cuda or t.device.index != self._device:
+            raise ValueError(f"{what} is on {t.device}, the context on cuda:{self._device}")
+        if dtype is not None and t.dtype != dtype:
+            raise ValueError(f"{what} is {t.dtype}, not {dtype}")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"{what} has the shape {tuple(t.shape)}, not {tuple(shape)}")
+        if not (_dense_rows(t) if rows else t.is_contiguous()):
+            raise ValueError(f"{what} has strides {t.stride()} that the call does not take")
+
+    def dropout(self, x, fx, p, fo=None, res=None, fres=None, mode=SR, seed=0, stream=0, out=None):
+        """Codes of format fx = (wl, fl) dropped with probability p and scaled by its counterpart, as codes of format fo
+        (default: fx), plus the codes `res` of format fres.  The gradient is the same call on the gradient's codes, with
+        the same p, seed and stream; mode is the rounding of the kept ones."""
+        fx = _fmt(fx)
+        fo = fx if fo is None else _fmt(fo)
+        self._own("x", x, dtype=self.storage_dtype(fx.wl))
+        if res is None:
+            fres = fx
+        else:
+            fres = _fmt(fres)
+            self._own("res", res, x.shape, self.storage_dtype(fres.wl))
+        if out is None:
+            out = self._torch.empty(x.shape, dtype=self.storage_dtype(fo.wl), device=x.device)
+        else:
+            self._own("out", out, x.shape, self.storage_dtype(fo.wl))
+        _check(self._lib.adapt_dropout(self._h, _ptr(x), fx, x.numel(), p, fo, Rng(mode, seed, stream), _ptr(res), fres, _ptr(out)),
+               "adapt_dropout")
+        return out
+
+    def _logits(self, logits, f):
+        """(format, rows, classes, row stride) of a matrix of logits: codes of format f, or fp32 (f = None)."""
+        f = _FP32 if f is None else _fmt(f)
+        if logits.dim() != 2:
+            raise ValueError(f"logits have the shape {tuple(logits.shape)}: rows x classes are wanted")
+        self._own("logits", logits, dtype=self.storage_dtype(f.wl) if f.wl else self._torch.float32, rows=True)
+        rows, classes = logits.shape
+        return f, rows, classes, _row_stride(logits)
+
+    def log_probs(self, logits, f, labels=None, topk=0, entropy=True):
+        """logits: rows x classes codes of format f = (wl, fl), or fp32 (f = None); a row may be longer than its classes
+        (stride(0) >= classes).  labels: int64[rows], negative where a row has none.  Returns dict(logp (None without
+        labels), lse, entropy (None unless asked for), top_idx int32[rows, topk], top_logp (None if topk = 0))."""
+        torch = self._torch
+        f, rows, classes, ld = self._logits(logits, f)
+        if labels is not None:
+            self._own("labels", labels, (rows,), torch.int64)
+        dev = logits.device
+        lse = torch.empty(rows, dtype=torch.float32, device=dev)
+        logp = torch.empty(rows, dtype=torch.float32, device=dev) if labels is not None else None
+        ent = torch.empty(rows, dtype=torch.float32, device=dev) if entropy else None
+        idx = torch.empty((rows, topk), dtype=torch.int32, device=dev) if topk > 0 else None
+        top = torch.empty((rows, topk), dtype=torch.float32, device=dev) if topk > 0 else None
+        _check(self._lib.adapt_log_probs(self._h, _ptr(logits), f, rows, classes, ld, _ptr(labels), _ptr(logp), _ptr(lse), _ptr(ent),
+                                         topk, _ptr(idx), _ptr(top)), "adapt_log_probs")
+        return {"logp": logp, "lse": lse, "entropy": ent, "top_idx": idx, "top_logp": top}
+
+    def cross_entropy(self, logits, f, labels, fg, weights=None, mode=SR, seed=0, stream=0, out=None):
+        """Softmax cross entropy of `logits` (as for log_probs) against labels (int64[rows], negative: row left out), rows
+        weighted by weights (fp32[rows] or None).  Returns (dlogits, logp): the gradient weights (p - onehot) as codes of
+        format fg = (wl, fl), what Net.backward takes with dlogits_fl = fl, and the labels' log probabilities."""
+        torch = self._torch
+        f, rows, classes, ld = self._logits(logits, f)
+        fg = _fmt(fg)
+        self._own("labels", labels, (rows,), torch.int64)
+        if weights is not None:
+            self._own("weights", weights, (rows,), torch.float32)
+        if out is None:
+            out = torch.empty((rows, classes), dtype=self.storage_dtype(fg.wl), device=logits.device)
+        else:
+            self._own("out", out, logits.shape, self.storage_dtype(fg.wl), rows=True)
+        logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        _check(self._lib.adapt_cross_entropy(self._h, _ptr(logits), f, rows, classes, ld, _ptr(labels), _ptr(weights), fg,
+                                             Rng(mode, seed, stream), _ptr(out), _row_stride(out), _ptr(logp)), "adapt_cross_entropy")
+        return out, logp
 
 
 class Net:

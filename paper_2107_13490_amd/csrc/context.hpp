@@ -94,6 +94,14 @@ inline size_t scratch_bytes(const adapt_ctx *c) { return c->ws_bytes - kCtlBytes
 inline uint32_t *ticket(adapt_ctx *c, int slot) { return reinterpret_cast<uint32_t *>(c->ws) + slot; }
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned_to(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+// the device that the context was created on is the one that a launch would go to now
+inline bool on_current_device(const adapt_ctx *c)
+{
+    int device = -1;
+    return hipGetDevice(&device) == hipSuccess && device == c->device;
+}
 
 inline int hip_status(adapt_ctx *c, hipError_t e)
 {
@@ -123,6 +131,9 @@ size_t ws_need_kld_search_batched(int num_cu, const adapt_kld_item *items, int c
 size_t ws_need_sgd_update(int num_cu, uint64_t n);
 size_t ws_need_gradient_diversity(uint64_t n, int count);
 size_t ws_need_requantize_fit(int num_cu, uint64_t n);
+size_t ws_need_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, adapt_fmt f);
+size_t ws_need_cross_entropy(int num_cu, uint64_t rows, uint64_t classes, adapt_fmt f, adapt_fmt fg);
+bool logits_ok(uint64_t rows, uint64_t classes, uint64_t ld);
 
 inline bool fmt_ok(adapt_fmt f) { return f.wl >= 2 && f.wl <= 16 && f.fl >= 0 && f.fl <= 31; }
 inline int storage_bytes(adapt_fmt f) { return f.wl <= 8 ? 1 : f.wl <= 16 ? 2 : 4; }      // int8, int16 or int32 codes

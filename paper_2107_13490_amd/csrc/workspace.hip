@@ -140,6 +140,13 @@ extern "C" size_t adapt_workspace_bytes(const adapt_ctx *ctx, const adapt_worksp
             return q->count < 1 ? kInvalid : ws_need_gradient_diversity(q->n, q->count) + slack;
         case ADAPT_CALL_REQUANTIZE_FIT:
             return ws_need_requantize_fit(num_cu, q->n) + slack;
+        case ADAPT_CALL_LOG_PROBS:
+            if (q->K < 1 || !logits_ok(q->n, q->K, q->K) || !(q->fa.wl == ADAPT_WL_FP32 || fmt_ok_wide(q->fa)) || q->count < 0 || q->count > 32 || q->count > q->K)
+                return kInvalid;
+            return ws_need_log_probs(num_cu, q->n, q->K, q->count, q->fa) + slack;
+        case ADAPT_CALL_CROSS_ENTROPY:
+            if (q->K < 1 || !logits_ok(q->n, q->K, q->K) || !(q->fa.wl == ADAPT_WL_FP32 || fmt_ok_wide(q->fa)) || !fmt_ok_wide(q->fb)) return kInvalid;
+            return ws_need_cross_entropy(num_cu, q->n, q->K, q->fa, q->fb) + slack;
         default:
             return kInvalid;
     }
