@@ -41,7 +41,131 @@ __device__ __forceinline__ long long drop_one(long long x, int up, int drop, int
     return q - (q * keep > t);                             // towards minus infinity
 }
 
-__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a)
+// ---- eight codes at any address of their element size (the device loads and stores unaligned vectors) ----
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int (&c)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(c, p, 32);
+    } else {
+        uint32_t w[2 * sizeof(T)];
+        __builtin_memcpy(w, p, sizeof(w));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            c[j] = sizeof(T) == 1 ? (int)(int8_t)(w[j >> 2] >> (8 * (j & 3))) : (int)(int16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const int (&c)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(p, c, 32);
+    } else {
+        uint32_t w[2 * sizeof(T)];
+#pragma unroll
+        for (int k = 0; k < (int)(2 * sizeof(T)); ++k)
+            w[k] = sizeof(T) == 1 ? (uint32_t)(c[4 * k] & 0xff) | ((uint32_t)(c[4 * k + 1] & 0xff) << 8) | ((uint32_t)(c[4 * k + 2] & 0xff) << 16) |
+                                        ((uint32_t)c[4 * k + 3] << 24)
+                                  : (uint32_t)(c[2 * k] & 0xffff) | ((uint32_t)c[2 * k + 1] << 16);
+        __builtin_memcpy(p, w, sizeof(w));
+    }
+}
+
+// What bounds it: 8-bit codes the vector units (a Philox block is 19 64-bit products and 20 three-way xors for 8 elements, 12 of
+// about 18 instruction slots each), wider ones memory.  33.5 M codes, us: 8 -> 8 bits 16.4 (4.1 TB/s), with an 8-bit residual
+// 24.6 (4.1), 16 -> 16 bits 27.1 (4.95; a copy on this card runs at 5.0).
+//
+// How floor((X + u)/K) is found; all of them exactly.  33.5 M codes of 8 bits, us: BY_TABLE 16.4, BY_F64 28.2; of 16 bits:
+// BY_I32 27.1, BY_F64 34.2.  The faster form is taken wherever it is exact.
+//   BY_TABLE  8-bit x: the quotient and the rest of X/K for each of its 256 values, in LDS.  An entry is q 2^16 + r with r + R
+//             carrying into the quotient where R is among the r largest draws, so that adding R to it rounds.
+//   BY_I32    |X + u| < 2^31, K >= 2^11: an fp32 quotient is off by less than one, and the rest says by what.
+//   BY_F64    |X + u| < 2^51: with a half added the sum is still exact, and its product with 1/K off by less than
+//             2^51 2^-52 / K, half of what separates it from a whole number.
+enum { BY_TABLE, BY_I32, BY_F64 };
+
+struct DropConst {
+    double d_up, d_inv, d_add;       // 2^up, 1/K, 1/2 and what makes R (nearest: 0) the u of the rule
+    float f_inv;
+    int drop, keep, up;
+};
+
+// RES: whether a residual is added, where that costs much (BY_F64 finds out by itself)
+template <typename TX, typename TO, int HOW, bool RES>
+__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a, const DropConst k)
+{
+    const TX *x = static_cast<const TX *>(a.x);
+    TO *out = static_cast<TO *>(a.out);
+    const double lo = -ldexp(1.0, a.wl - 1), hi = ldexp(1.0, a.wl - 1) - 1.0;
+    const int ilo = (int)lo, ihi = (int)hi;
+    const double res_scale = ldexp(1.0, a.res_up);
+    const bool has_res = HOW == BY_F64 ? a.res != nullptr : RES, nearest = HOW == BY_F64 && a.mode != ADAPT_SR;
+    __shared__ uint32_t table[HOW == BY_TABLE ? 256 : 1];
+    if constexpr (HOW == BY_TABLE) {
+        static_assert(kDropThreads == 256, "an entry per thread");
+        const double X = (double)(int8_t)threadIdx.x * k.d_up;
+        int q = (int)floor((X + 0.5) * k.d_inv);
+        int r = (int)(X - (double)q * (double)k.keep);
+        if (!RES && (q < ilo || q >= ihi)) { q = q < ilo ? ilo : ihi; r = 0; }        // saturated here where nothing is added
+        table[threadIdx.x] = ((uint32_t)q << 16) | (uint32_t)r;
+        __syncthreads();
+    }
+    auto one = [&](int c, int res, uint32_t r16) -> int {
+        const bool stays = (int)r16 >= k.drop;
+        int q;
+        if constexpr (HOW == BY_TABLE) {
+            q = (int)(table[c & 255] + r16) >> 16;
+        } else if constexpr (HOW == BY_I32) {
+            const int n = (int)(((uint32_t)c << k.up) + r16) - k.drop;
+            q = (int)floorf((float)n * k.f_inv);
+            const int rest = n - __mul24(q, k.keep);
+            q += (rest >= k.keep) - (rest < 0);
+        } else {
+            double y = floor(fma((double)c, k.d_up, (nearest ? 0.0 : (double)r16) + k.d_add) * k.d_inv);
+            y = stays ? y : 0.0;
+            if (has_res) y += (double)res * res_scale;                   // beyond 2^53 it saturates, rounded or not
+            return (int)fmin(fmax(y, lo), hi);
+        }
+        q = stays ? q : 0;
+        if (RES) q += (int)((uint32_t)res << a.res_up);
+        return HOW == BY_TABLE && !RES ? q : min(max(q, ilo), ihi);
+    };
+    auto residual = [&](uint64_t g, int (&r)[8]) {
+        if (a.es_res == 1) load8(static_cast<const int8_t *>(a.res) + 8 * g, r);
+        else if (a.es_res == 2) load8(static_cast<const int16_t *>(a.res) + 8 * g, r);
+        else load8(static_cast<const int32_t *>(a.res) + 8 * g, r);
+    };
+    auto group = [&](uint64_t g, const int (&c)[8], const int (&r)[8]) {
+        const u32x4 blk = rounding_block(a.seed, a.stream, g);
+        int v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = one(c[e], r[e], lane16(blk, e));
+        store8(out + 8 * g, v);
+    };
+    const uint64_t full = a.n >> 3, stride = (uint64_t)gridDim.x * kDropThreads;
+    uint64_t g = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x;
+    for (; g + stride < full; g += 2 * stride) {
+        int c0[8], c1[8], r0[8] = {}, r1[8] = {};
+        load8(x + 8 * g, c0);
+        load8(x + 8 * (g + stride), c1);
+        if (has_res) { residual(g, r0); residual(g + stride, r1); }
+        group(g, c0, r0);
+        group(g + stride, c1, r1);
+    }
+    if (g < full) {
+        int c[8], r[8] = {};
+        load8(x + 8 * g, c);
+        if (has_res) residual(g, r);
+        group(g, c, r);
+        g += stride;
+    }
+    if (g == full)                                         // the last, incomplete group has an owner too
+        for (uint64_t i = full << 3; i < a.n; ++i)
+            out[i] = (TO)one(x[i], has_res ? (int)code_at(a.res, a.es_res, i) : 0, rounding_bits_of(a.seed, a.stream, i, ADAPT_SR));
+}
+
+// X beyond 2^50: 64-bit integers
+__global__ void __launch_bounds__(kDropThreads) dropout_i64_kernel(const DropArgs a)
 {
     const long long hi = (1ll << (a.wl - 1)) - 1, lo = -hi - 1;
     for (uint64_t i = (uint64_t)blockIdx.x * kDropThreads + threadIdx.x; i < a.n; i += (uint64_t)gridDim.x * kDropThreads) {
@@ -59,6 +183,15 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a)
 
 using namespace adapt;
 
+template <typename TX, int HOW, bool RES>
+static void launch(adapt_ctx *ctx, dim3 grid, const DropArgs &a, const DropConst &k)
+{
+    const dim3 block(kDropThreads);
+    if (a.es_o == 1) hipLaunchKernelGGL((dropout_kernel<TX, int8_t, HOW, RES>), grid, block, 0, ctx->stream, a, k);
+    else if (a.es_o == 2) hipLaunchKernelGGL((dropout_kernel<TX, int16_t, HOW, RES>), grid, block, 0, ctx->stream, a, k);
+    else hipLaunchKernelGGL((dropout_kernel<TX, int32_t, HOW, RES>), grid, block, 0, ctx->stream, a, k);
+}
+
 extern "C" int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t n, double p, adapt_fmt fo, adapt_rng rng,
                              const void *res, adapt_fmt fres, void *out)
 {
@@ -71,8 +204,25 @@ extern "C" int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t
     if (n == 0) return ADAPT_OK;
     const int es_x = storage_bytes(fx), es_o = storage_bytes(fo), es_r = res ? storage_bytes(fres) : 1;
     if (!x || !out || !aligned_to(x, es_x) || !aligned_to(out, es_o) || !aligned_to(res, es_r)) return ADAPT_EINVAL;
-    DropArgs a = {x, res, out, n, 16 + fo.fl - fx.fl, res ? fo.fl - fres.fl : 0, drop, 65536 - drop, es_x, es_r, es_o, fo.wl, rng.mode, rng.seed, rng.stream};
-    const int grid = (int)std::min<uint64_t>((n + kDropThreads - 1) / kDropThreads, (uint64_t)ctx->num_cu * 8);
-    hipLaunchKernelGGL(dropout_kernel, dim3(grid), dim3(kDropThreads), 0, ctx->stream, a);
+    const int up = 16 + fo.fl - fx.fl, keep = 65536 - drop;
+    const DropArgs a = {x, res, out, n, up, res ? fo.fl - fres.fl : 0, drop, keep, es_x, es_r, es_o, fo.wl, rng.mode, rng.seed, rng.stream};
+    const bool nearest = rng.mode != ADAPT_SR;
+    const DropConst k = {std::ldexp(1.0, up), 1.0 / keep, 0.5 + (nearest ? keep >> 1 : -drop), 1.0f / (float)keep, drop, keep, up};
+    const uint64_t groups = (n + 7) >> 3;
+    const dim3 grid((unsigned)std::min<uint64_t>((groups + kDropThreads - 1) / kDropThreads, (uint64_t)ctx->num_cu * 8)), block(kDropThreads);
+    const bool in_32 = !nearest && (!res || fres.wl - 1 + a.res_up <= 29);      // the residual and its sum with a quotient
+    const bool table = in_32 && fx.wl <= 8 && up >= 0 && std::ldexp(1.0, fx.wl - 1 + up) < 32767.0 * keep;
+    const bool i32 = in_32 && fx.wl <= 16 && up >= 0 && fx.wl - 1 + up <= 30 && keep >= 2048;
+    if (up < 0 || fx.wl - 1 + up > 50) hipLaunchKernelGGL(dropout_i64_kernel, grid, block, 0, ctx->stream, a);
+    else if (fx.wl > 16) launch<int32_t, BY_F64, true>(ctx, grid, a, k);
+    else if (fx.wl > 8) {
+        if (!i32) launch<int16_t, BY_F64, true>(ctx, grid, a, k);
+        else if (res) launch<int16_t, BY_I32, true>(ctx, grid, a, k);
+        else launch<int16_t, BY_I32, false>(ctx, grid, a, k);
+    } else {
+        if (!table) launch<int8_t, BY_F64, true>(ctx, grid, a, k);
+        else if (res) launch<int8_t, BY_TABLE, true>(ctx, grid, a, k);
+        else launch<int8_t, BY_TABLE, false>(ctx, grid, a, k);
+    }
     return hip_status(ctx, hipGetLastError());
 }
