@@ -127,34 +127,289 @@ __global__ void __launch_bounds__(kRowThreads) log_probs_kernel(const LogitArgs 
     }
 }
 
-template <typename T, typename G>
-__global__ void __launch_bounds__(kRowThreads) cross_entropy_kernel(const LogitArgs a)
+// ---------------------------------------------------------------------------------------------
+// Cross entropy.  A block takes a row, or one chunk of a long one: the largest logit (int16 and wider), the sum of the
+// exponentials, the codes.  Only the first sweep reads memory, the others find the row in the caches.  Elements come in units
+// that start where the generator's blocks of eight start, so that a unit takes whole blocks whatever the number of classes; in
+// a dense tensor units are aligned vectors, too.  What a row has before its first and behind its last whole unit are its edges,
+// one element per thread.
+// ---------------------------------------------------------------------------------------------
+template <typename T> constexpr int kUnit = sizeof(T) == 1 ? 16 : 8;      // elements
+template <typename T> constexpr int kWords = kUnit<T> * (int)sizeof(T) / 4;
+constexpr int kMostThreads = 1024;
+
+template <typename T>
+__device__ __forceinline__ T unit_get(const uint32_t (&w)[kWords<T>], int e)
 {
-    const double qmin = -ldexp(1.0, a.wl_g - 1), qmax = ldexp(1.0, a.wl_g - 1) - 1.0;
-    for (uint64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
-        const T *row = static_cast<const T *>(a.logits) + i * a.ld;
-        G *grad = static_cast<G *>(a.grad) + i * a.ldg;
-        const RowStats r = row_stats(row, a.classes, a.fl);
-        const int64_t label = a.labels[i];
-        if (threadIdx.x == 0 && a.logp) a.logp[i] = label_log_prob(row, label, a.classes, a.fl, r);
-        const bool counts = label >= 0 && (uint64_t)label < a.classes && r.m > -INFINITY;
-        const double scale = counts ? (a.weights ? (double)a.weights[i] : 1.0) * ldexp(1.0, a.fl_g) / r.s : 0.0;
-        for (uint64_t j = threadIdx.x; j < a.classes; j += kRowThreads) {
-            long long q = 0;
-            if (counts) {
-                double t = exp(value_of(row[j], a.fl) - r.m);
-                if (j == (uint64_t)label) t -= r.s;
-                const double y = fmin(fmax(t * scale, qmin), qmax);
-                q = ((long long)floor(y * 65536.0) + (long long)rounding_bits_of(a.seed, a.stream, i * a.classes + j, a.mode)) >> 16;
-                q = q > (long long)qmax ? (long long)qmax : q;
-            }
-            grad[j] = (G)q;
-        }
-    }
+    if constexpr (sizeof(T) == 1) return (T)(w[e >> 2] >> (8 * (e & 3)));
+    else if constexpr (sizeof(T) == 2) return (T)(w[e >> 1] >> (16 * (e & 1)));
+    else return __builtin_bit_cast(T, w[e]);
 }
 
+// exp in fp64 of a number of at most 700: 2^(n/256) e^r, |r| <= ln 2 / 512, with a table of the 256 roots and four terms (the
+// next is 4e-17).  Below -700 the result is some number below 1e-300.
+__device__ __forceinline__ double exp_by_roots(double d, const double *roots)
+{
+    d = fmax(d, -700.0);
+    const double shifted = fma(d, 369.32993046757462711, 6755399441055744.0);      // 256 / ln 2; 1.5 2^52 leaves n in the low word
+    const int n = __double2loint(shifted);
+    const double r = fma(shifted - 6755399441055744.0, -0.0027076061740622863, d); // ln 2 / 256
+    double p = fma(r, 1.0 / 24.0, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    p *= roots[n & 255];
+    return __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
+}
+
+// The exponentials of one type of logits relative to a reference, as each block sets them up in LDS.
+//   int8     e^x for each code; the reference is 0 (|x| <= 128)
+//   int16    e^-d = hi[d >> 8] lo[d & 255] for the distance d of a code to the reference
+//   others   exp_by_roots of the distance
+// The reference of int16 and int32 is the largest code of the format where the whole range of distances is below 700, so that
+// no exponential vanishes; otherwise, the largest of the row.
+template <typename T>
+struct Exponentials {
+    static constexpr int kTable = sizeof(T) == 1 ? 256 : sizeof(T) == 2 ? 512 : 256;
+    const double *table;
+    int fl;
+    double step;      // 2^-fl
+
+    __device__ __forceinline__ static void build(double *table, int fl)
+    {
+        const double step = ldexp(1.0, -fl);
+        for (int j = threadIdx.x; j < kTable; j += blockDim.x) {
+            if constexpr (sizeof(T) == 1) table[j] = exp((double)(int8_t)j * step);
+            else if constexpr (sizeof(T) == 2) table[j] = exp(-(double)(j < 256 ? j << 8 : j - 256) * step);
+            else table[j] = exp2((double)j / 256.0);
+        }
+    }
+    __device__ __forceinline__ double at(T l, T m) const
+    {
+        if constexpr (sizeof(T) == 1) return table[(uint8_t)l];
+        else if constexpr (sizeof(T) == 2) {
+            const uint32_t d = (uint32_t)((int)m - (int)l);
+            return table[d >> 8] * table[256 + (d & 255)];
+        } else if constexpr (__is_same(T, float)) return exp_by_roots((double)l - (double)m, table);
+        else return exp_by_roots((double)((long long)l - m) * step, table);
+    }
+};
+
+template <typename T> __device__ __forceinline__ T lowest() { return (T)(sizeof(T) == 1 ? -128 : sizeof(T) == 2 ? -32768 : INT32_MIN); }
+template <> __device__ __forceinline__ float lowest<float>() { return -INFINITY; }
+template <typename T> __device__ __forceinline__ T larger(T a, T b) { return a > b ? a : b; }
+template <> __device__ __forceinline__ float larger<float>(float a, float b) { return fmaxf(a, b); }
+
+// reduction over the block; `part` is used once
+template <typename V, typename Op>
+__device__ __forceinline__ V over_block(V v, V *part, Op op)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = op(v, (V)__shfl_xor(v, off, 64));
+    if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+    for (int w = 1; w < (int)(blockDim.x / kWave); ++w) v = op(v, part[w]);
+    return v;
+}
+
+struct RowPart { double m, s; };      // largest value (0: not needed) and sum of a chunk
+
+enum { WHOLE_ROW, CHUNK_SUMS, CHUNK_CODES };
+struct ChunkArgs {
+    uint32_t splits, units;           // chunks of a row, units of a chunk
+    RowPart *part;                    // [row][chunk]
+    bool fixed;                       // the reference is the code `top`
+    int top;
+};
+
+template <typename T>
+__device__ __forceinline__ void load_unit(const T *p, uint32_t (&w)[kWords<T>]) { __builtin_memcpy(w, p, kUnit<T> * sizeof(T)); }
+
+template <typename T, typename G, int MODE>
+__global__ void __launch_bounds__(kMostThreads) cross_entropy_kernel(const LogitArgs a, const ChunkArgs c)
+{
+    constexpr int U = kUnit<T>, W = kWords<T>;
+    constexpr bool kByte = sizeof(T) == 1, kFloat = __is_same(T, float);
+    using X = Exponentials<T>;
+    __shared__ double table[X::kTable];
+    __shared__ double part_s[kMostThreads / kWave];
+    __shared__ T part_m[kMostThreads / kWave];
+    __shared__ int64_t codes64[kByte && sizeof(G) == 4 ? 256 : 1];
+    __shared__ int32_t codes32[kByte && sizeof(G) < 4 ? 256 : 1];
+    const uint64_t i = blockIdx.x / c.splits;
+    const uint32_t chunk = blockIdx.x - (uint32_t)i * c.splits;
+    const T *row = static_cast<const T *>(a.logits) + i * a.ld;
+    const uint64_t base = i * a.classes;
+    const uint32_t head = (uint32_t)min((uint64_t)(-base & (U - 1)), a.classes);
+    const uint64_t whole = (a.classes - head) / U, first = min((uint64_t)chunk * c.units, whole);
+    const uint32_t units = (uint32_t)min(whole - first, (uint64_t)c.units), tail = (uint32_t)(a.classes - head - whole * U);
+    const T *body = row + head + first * U;
+    // the edges belong to the first chunk
+    const bool on_edge = chunk == 0 && threadIdx.x < head + tail;
+    const uint64_t edge_col = threadIdx.x < head ? threadIdx.x : a.classes - (head + tail) + threadIdx.x;
+    const T edge = on_edge ? row[edge_col] : lowest<T>();
+    G *grad = static_cast<G *>(a.grad) + i * a.ldg;
+    const int64_t label = a.labels[i];
+    const bool there = label >= 0 && (uint64_t)label < a.classes;
+    const auto no_gradient = [&](float logp) {
+        G zero[U] = {};
+        for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) __builtin_memcpy(grad + head + (first + u) * U, zero, sizeof(zero));
+        if (on_edge) grad[edge_col] = 0;
+        if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = logp;
+    };
+    if (!there) {                                             // such a row is not read
+        if (MODE != CHUNK_SUMS) no_gradient(label < 0 ? 0.0f : NAN);
+        return;
+    }
+
+    X::build(table, a.fl);
+    const X ex = {table, a.fl, ldexp(1.0, -a.fl)};
+    T m = (T)c.top;
+    if (!kByte && !kFloat && !c.fixed && MODE != CHUNK_CODES) {
+        m = edge;
+        for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+            uint32_t w[W];
+            load_unit(body + (uint64_t)u * U, w);
+#pragma unroll
+            for (int e = 0; e < U; ++e) m = larger(m, unit_get<T>(w, e));
+        }
+        m = over_block(m, part_m, [](T x, T y) { return larger(x, y); });
+    } else {
+        __syncthreads();
+    }
+
+    double ref, sum;
+    const auto add = [](double x, double y) { return x + y; };
+    if constexpr (MODE != CHUNK_CODES) {
+        double s = 0.0;
+        if constexpr (kFloat) {
+            // every thread has a reference of its own, which follows the logits only where they get 600 ahead of it
+            float r = -INFINITY;
+            int bad = 0;
+            const auto take = [&](float largest) -> bool {
+                if (!(largest < INFINITY)) { bad = 1; return false; }
+                if (largest > r + 600.0f) { s = r > -INFINITY ? s * exp((double)r - (double)largest) : 0.0; r = largest; }
+                return largest > -INFINITY;
+            };
+            if (on_edge && take(edge)) s += ex.at(edge, r);
+            for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+                uint32_t w[W];
+                load_unit(body + (uint64_t)u * U, w);
+                float largest = unit_get<T>(w, 0);
+#pragma unroll
+                for (int e = 1; e < U; ++e) largest = __builtin_elementwise_maximum(largest, unit_get<T>(w, e));
+                if (!take(largest)) continue;
+#pragma unroll
+                for (int e = 0; e < U; ++e) s += ex.at(unit_get<T>(w, e), r);
+            }
+            m = over_block(r, part_m, [](T x, T y) { return larger(x, y); });
+            s = r > -INFINITY ? s * exp((double)r - (double)m) : 0.0;
+            if (__syncthreads_or(bad)) s = NAN;
+        } else {
+            if (on_edge) s = ex.at(edge, m);
+            for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+                uint32_t w[W];
+                load_unit(body + (uint64_t)u * U, w);
+#pragma unroll
+                for (int e = 0; e < U; ++e) s += ex.at(unit_get<T>(w, e), m);
+            }
+        }
+        sum = over_block(s, part_s, add);
+        ref = kByte ? 0.0 : value_of(m, a.fl);
+        if constexpr (MODE == CHUNK_SUMS) {
+            if (threadIdx.x == 0) c.part[blockIdx.x] = {ref, sum};
+            return;
+        }
+    } else {
+        __shared__ double part_r[kMostThreads / kWave];
+        const RowPart *p = c.part + i * c.splits;
+        double s = 0.0;
+        ref = -INFINITY;
+        for (uint32_t j = threadIdx.x; j < c.splits; j += blockDim.x) ref = fmax(ref, p[j].m);
+        ref = over_block(ref, part_r, [](double x, double y) { return fmax(x, y); });
+        for (uint32_t j = threadIdx.x; j < c.splits; j += blockDim.x) s += p[j].m > -INFINITY ? p[j].s * exp(p[j].m - ref) : p[j].s;
+        sum = over_block(s, part_s, add);
+        if constexpr (!kByte) m = kFloat ? (T)ref : (T)ldexp(ref, a.fl);
+    }
+
+    if (sum != sum || ref == -INFINITY) {
+        no_gradient(sum != sum ? NAN : -INFINITY);
+        return;
+    }
+    if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = (float)(value_of(row[label], a.fl) - ref - log(sum));
+    // floor of the clamped value in units of 2^-16 of a code, and the code for a draw
+    const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0;
+    const double scale = (a.weights ? (double)a.weights[i] : 1.0) * ldexp(1.0, a.fl_g + 16) / sum;
+    const auto grid_of = [&](double t) { return floor(fmin(fmax(t * scale, tmin), tmax)); };
+    const auto code_of = [](double z, uint32_t r16) -> int {
+        if constexpr (sizeof(G) == 4) return (int)(((long long)z + r16) >> 16);
+        else return ((int)z + (int)r16) >> 16;
+    };
+    if constexpr (kByte) {
+        for (int j = threadIdx.x; j < 256; j += blockDim.x) {
+            if constexpr (sizeof(G) == 4) codes64[j] = (int64_t)grid_of(table[j]);
+            else codes32[j] = (int32_t)grid_of(table[j]);
+        }
+        __syncthreads();
+    }
+    const auto code_at = [&](T l, uint32_t r16) -> G {
+        if constexpr (kByte && sizeof(G) == 4) return (G)((codes64[(uint8_t)l] + (int)r16) >> 16);
+        else if constexpr (kByte) return (G)((codes32[(uint8_t)l] + (int)r16) >> 16);
+        else return (G)code_of(grid_of(ex.at(l, m)), r16);
+    };
+    const uint64_t group0 = (base + head) / 8 + first * (U / 8);
+    for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+        uint32_t w[W];
+        load_unit(body + (uint64_t)u * U, w);
+        G q[U];
+#pragma unroll
+        for (int h = 0; h < U / 8; ++h) {
+            u32x4 blk = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+            if (a.mode == ADAPT_SR) blk = rounding_block(a.seed, a.stream, group0 + (uint64_t)u * (U / 8) + h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[8 * h + e] = code_at(unit_get<T>(w, 8 * h + e), lane16(blk, e));
+        }
+        __builtin_memcpy(grad + head + (first + u) * U, q, sizeof(q));
+    }
+    if (on_edge) grad[edge_col] = code_at(edge, rounding_bits_of(a.seed, a.stream, base + edge_col, a.mode));
+    // the label's own element, by the thread that has just stored it among others
+    const int64_t at = label - (int64_t)head - (int64_t)(first * U);
+    const bool mine = at >= 0 && at < (int64_t)units * U ? (uint32_t)(at / U) % blockDim.x == threadIdx.x : on_edge && edge_col == (uint64_t)label;
+    if (mine) grad[label] = (G)code_of(grid_of(ex.at(row[label], m) - sum), rounding_bits_of(a.seed, a.stream, base + (uint64_t)label, a.mode));
+}
+
+
 size_t ws_need_log_probs(int, uint64_t, uint64_t, int, adapt_fmt) { return 16; }
-size_t ws_need_cross_entropy(int, uint64_t, uint64_t, adapt_fmt, adapt_fmt) { return 16; }
+
+// How the rows of a cross entropy are cut: rows too few to fill the card into chunks, whose sums are a launch of their own.
+struct CrossEntropyPlan {
+    uint32_t splits, units, threads;
+    size_t ws_bytes;
+};
+
+static CrossEntropyPlan plan_cross_entropy(int num_cu, uint64_t rows, uint64_t classes, adapt_fmt f)
+{
+    const int U = f.wl != ADAPT_WL_FP32 && f.wl <= 8 ? 16 : 8;
+    CrossEntropyPlan p = {};
+    const uint64_t all = std::max<uint64_t>(classes / U, 1);
+    uint64_t splits = 1;
+    const uint64_t wanted = 4 * (uint64_t)num_cu;             // blocks
+    if (rows < wanted / 2 && all >= 512) splits = std::min<uint64_t>((wanted + rows - 1) / std::max<uint64_t>(rows, 1), all / 256);
+    p.splits = (uint32_t)splits;
+    p.units = (uint32_t)((all + splits - 1) / splits);
+    // units per thread, us (rows x classes, bits; 256, 512, 1024 threads): 8192 x 32000, 8: 140, 151, 190; 1536 x 65531, 16: 186, 157,
+    // 163; 2048 x 32000, 24: 169, 157, 174; 1024 x 50001, fp32: 129, 125, 126; with few rows more threads: 512 x 32000, 8: 15.6, 13.8, 14.6
+    const uint64_t per = rows * splits >= wanted ? 8 : 4, threads = (p.units + per - 1) / per;
+    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, 512);
+    p.ws_bytes = p.splits > 1 ? rows * p.splits * sizeof(RowPart) : 0;
+    return p;
+}
+
+size_t ws_need_cross_entropy(int num_cu, uint64_t rows, uint64_t classes, adapt_fmt f, adapt_fmt)
+{
+    return plan_cross_entropy(num_cu, rows, classes, f).ws_bytes + 16;
+}
 
 bool logits_ok(uint64_t rows, uint64_t classes, uint64_t ld)
 {
@@ -192,13 +447,26 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     return hip_status(ctx, hipGetLastError());
 }
 
-template <typename T>
-static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a)
+template <typename T, typename G>
+static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
 {
-    const dim3 grid((unsigned)std::min<uint64_t>(a.rows, 1u << 20)), block(kRowThreads);
-    if (a.wl_g <= 8) hipLaunchKernelGGL((cross_entropy_kernel<T, int8_t>), grid, block, 0, ctx->stream, a);
-    else if (a.wl_g <= 16) hipLaunchKernelGGL((cross_entropy_kernel<T, int16_t>), grid, block, 0, ctx->stream, a);
-    else hipLaunchKernelGGL((cross_entropy_kernel<T, int32_t>), grid, block, 0, ctx->stream, a);
+    // distances to the largest code: of the storage for int16 (they index tables), of the format for int32
+    const int span = sizeof(T) == 2 ? 16 : wl;
+    const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), span - a.fl <= 9, (int)((1ll << (span - 1)) - 1)};
+    const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
+    if (p.splits == 1) {
+        hipLaunchKernelGGL((cross_entropy_kernel<T, G, WHOLE_ROW>), grid, block, 0, ctx->stream, a, c);
+    } else {
+        hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_SUMS>), grid, block, 0, ctx->stream, a, c);
+        hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_CODES>), grid, block, 0, ctx->stream, a, c);
+    }
+}
+template <typename T>
+static void launch_cross_entropy_to(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
+{
+    if (a.wl_g <= 8) launch_cross_entropy<T, int8_t>(ctx, a, p, wl);
+    else if (a.wl_g <= 16) launch_cross_entropy<T, int16_t>(ctx, a, p, wl);
+    else launch_cross_entropy<T, int32_t>(ctx, a, p, wl);
 }
 
 extern "C" int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes, size_t ld, const int64_t *labels,
@@ -219,9 +487,12 @@ extern "C" int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt
     a.labels = labels; a.logp = logp; a.weights = weights;
     a.grad = dlogits; a.ldg = ldg;
     a.wl_g = fg.wl; a.fl_g = fg.fl; a.mode = rng.mode; a.seed = rng.seed; a.stream = rng.stream;
-    if (f.wl == ADAPT_WL_FP32) launch_cross_entropy<float>(ctx, a);
-    else if (f.wl <= 8) launch_cross_entropy<int8_t>(ctx, a);
-    else if (f.wl <= 16) launch_cross_entropy<int16_t>(ctx, a);
-    else launch_cross_entropy<int32_t>(ctx, a);
+    const CrossEntropyPlan p = plan_cross_entropy(ctx->num_cu, rows, classes, f);
+    if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
+    if (rows * p.splits >= (1ull << 31)) return ADAPT_EUNSUPPORTED;
+    if (f.wl == ADAPT_WL_FP32) launch_cross_entropy_to<float>(ctx, a, p, 0);
+    else if (f.wl <= 8) launch_cross_entropy_to<int8_t>(ctx, a, p, f.wl);
+    else if (f.wl <= 16) launch_cross_entropy_to<int16_t>(ctx, a, p, f.wl);
+    else launch_cross_entropy_to<int32_t>(ctx, a, p, f.wl);
     return hip_status(ctx, hipGetLastError());
 }
