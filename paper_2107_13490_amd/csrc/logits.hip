@@ -7,7 +7,6 @@
 
 namespace adapt {
 
-constexpr int kRowThreads = 256;
 constexpr int kMaxTop = 32;
 
 struct LogitArgs {
@@ -30,102 +29,16 @@ struct LogitArgs {
 template <typename T>
 __device__ __forceinline__ double value_of(T l, int fl) { return ldexp((double)l, -fl); }
 
-// a logit's place among those of its row: larger first, then the lower index
-template <typename T>
-__device__ __forceinline__ uint64_t key_of(T l, uint32_t j) { return ((uint64_t)((uint32_t)(int32_t)l ^ 0x80000000u) << 32) | (0x7fffffffu - j); }
-template <>
-__device__ __forceinline__ uint64_t key_of<float>(float l, uint32_t j)
+// The order of logits as that of 32-bit numbers: a NaN counts as -inf, -0 as 0
+__device__ __forceinline__ uint32_t order_of(int v) { return (uint32_t)v ^ 0x80000000u; }
+__device__ __forceinline__ uint32_t order_of(float v)
 {
-    const float v = l != l ? -INFINITY : l == 0.0f ? 0.0f : l;
+    v = v != v ? -INFINITY : v == 0.0f ? 0.0f : v;
     const uint32_t b = __float_as_uint(v);
-    return ((uint64_t)((b & 0x80000000u) ? ~b : b | 0x80000000u) << 32) | (0x7fffffffu - j);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-
-template <typename V, typename Op>
-__device__ __forceinline__ V block_reduce(V v, Op op)
-{
-    __shared__ V part[kRowThreads / kWave];
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off, 64));
-    if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = part[0];
-    for (int w = 1; w < kRowThreads / kWave; ++w) v = op(v, part[w]);
-    __syncthreads();
-    return v;
-}
-
-// largest value of a row (-inf: no class possible; NaN: a NaN or +inf among the logits) and the sums of exp(x - m) and (x - m) exp(x - m)
-struct RowStats { double m, s, e; };
-
-template <typename T>
-__device__ __forceinline__ RowStats row_stats(const T *row, uint64_t classes, int fl)
-{
-    RowStats r;
-    double m = -INFINITY;
-    int bad = 0;
-    for (uint64_t j = threadIdx.x; j < classes; j += kRowThreads) {
-        const double x = value_of(row[j], fl);
-        bad |= !(x < INFINITY);
-        m = fmax(m, x);
-    }
-    r.m = block_reduce(m, [](double a, double b) { return fmax(a, b); });
-    if (block_reduce(bad, [](int a, int b) { return a | b; })) r.m = NAN;
-    r.s = r.e = 0.0;
-    for (uint64_t j = threadIdx.x; j < classes; j += kRowThreads) {
-        const double d = value_of(row[j], fl) - r.m;
-        if (!(d > -INFINITY)) continue;
-        const double t = exp(d);
-        r.s += t;
-        r.e += t * d;
-    }
-    const auto add = [](double a, double b) { return a + b; };
-    r.s = block_reduce(r.s, add);
-    r.e = block_reduce(r.e, add);
-    return r;
-}
-
-__device__ __forceinline__ float log_prob(double x, const RowStats &r)
-{
-    return r.m == -INFINITY ? -INFINITY : (float)(x - r.m - log(r.s));
-}
-
-template <typename T>
-__device__ __forceinline__ float label_log_prob(const T *row, int64_t label, uint64_t classes, int fl, const RowStats &r)
-{
-    if (label < 0) return 0.0f;
-    if ((uint64_t)label >= classes || r.m != r.m) return NAN;
-    return log_prob(value_of(row[label], fl), r);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) log_probs_kernel(const LogitArgs a)
-{
-    for (uint64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
-        const T *row = static_cast<const T *>(a.logits) + i * a.ld;
-        const RowStats r = row_stats(row, a.classes, a.fl);
-        if (threadIdx.x == 0) {
-            const bool none = r.m == -INFINITY;
-            if (a.lse) a.lse[i] = none ? -INFINITY : (float)(r.m + log(r.s));
-            if (a.entropy) a.entropy[i] = r.m != r.m ? NAN : none ? 0.0f : (float)(log(r.s) - r.e / r.s);
-            if (a.logp) a.logp[i] = label_log_prob(row, a.labels[i], a.classes, a.fl, r);
-        }
-        uint64_t last = ~0ull;
-        for (int k = 0; k < a.topk; ++k) {
-            uint64_t best = 0;
-            for (uint64_t j = threadIdx.x; j < a.classes; j += kRowThreads) {
-                const uint64_t key = key_of(row[j], (uint32_t)j);
-                if (key < last && key > best) best = key;
-            }
-            last = block_reduce(best, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-            if (threadIdx.x == 0) {
-                const uint32_t j = 0x7fffffffu - (uint32_t)last;
-                a.top_index[i * a.topk + k] = (int32_t)j;
-                a.top_logp[i * a.topk + k] = r.m != r.m ? NAN : log_prob(value_of(row[j], a.fl), r);
-            }
-        }
-    }
-}
+// larger first, then the lower index; never 0 (indices are below 2^30)
+__device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) { return ((uint64_t)order << 32) | (0x7fffffffu - index); }
 
 // ---------------------------------------------------------------------------------------------
 // Cross entropy.  A block takes a row, or one chunk of a long one: the largest logit (int16 and wider), the sum of the
@@ -380,7 +293,342 @@ __global__ void __launch_bounds__(kMostThreads) cross_entropy_kernel(const Logit
 }
 
 
-size_t ws_need_log_probs(int, uint64_t, uint64_t, int, adapt_fmt) { return 16; }
+// ---------------------------------------------------------------------------------------------
+// Log probabilities.  One sweep over the row (or a chunk of it): sums of e^(x - r) and (x - r) e^(x - r) in fp32 over a unit and in
+// fp64 from there on, and each thread's largest unit.  Where all of the format's values lie within +-16, r = 0; otherwise every
+// thread has a reference of its own that follows the logits where they get 8 ahead of it.
+// The k largest: the threads fall into 64 groups (their lanes), and the k-th largest of the groups' maxima is a bound below
+// which none of them lies.  Few threads have anything above it; those look through their units again and put what they find
+// into a list, whose members count how many are ahead of them.  Should the list overflow (the largest logits in few places,
+// many of them), the row is swept once for each of the k.
+// ---------------------------------------------------------------------------------------------
+struct LogPart { double r, s, e; };      // reference (fp64 values; NaN: not a distribution), sums of a chunk
+
+struct LogChunkArgs {
+    uint32_t splits, units;
+    LogPart *part;                       // [row][chunk]
+    uint64_t *keys;                      // [row][chunk][topk]
+    int listed;                          // entries of the list
+    bool fixed;                          // r = 0
+};
+
+template <typename T> struct RowValue { typedef float type; };      // 8- and 16-bit codes are exact in fp32
+template <> struct RowValue<int32_t> { typedef int type; };
+
+// scratch of the selection, in LDS
+struct TopScratch {
+    uint64_t bound;
+    uint32_t count;
+    uint32_t ahead[kWave];      // groups ahead of this one, and (16 bits up) those not behind it
+    uint64_t group[kWave];
+    uint64_t best[kMaxTop];
+    uint64_t part[kMostThreads / kWave];
+};
+
+// The bound for the k largest from one key per thread (0: none); scratch.count = 0 afterwards
+__device__ __forceinline__ uint64_t bound_of(uint64_t key, int k, TopScratch &s, uint64_t *list)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    list[threadIdx.x] = key;
+    if (threadIdx.x < kWave) s.ahead[lane] = 0;
+    if (threadIdx.x == 0) { s.bound = 0; s.count = 0; }
+    __syncthreads();
+    if (wave == 0) {
+        for (int w = 1; w < waves; ++w) { const uint64_t o = list[w * kWave + lane]; key = o > key ? o : key; }
+        s.group[lane] = key;
+    }
+    __syncthreads();
+    key = s.group[lane];
+    uint32_t ahead = 0;
+    for (int j = wave; j < kWave; j += waves) ahead += (s.group[j] > key ? 0x10001u : 0u) + (s.group[j] == key ? 0x10000u : 0u);
+    atomicAdd(&s.ahead[lane], ahead);
+    __syncthreads();
+    ahead = s.ahead[lane];
+    if (wave == 0 && (int)(ahead & 0xffff) < k && (int)(ahead >> 16) >= k) s.bound = key;      // the same from every such lane
+    __syncthreads();
+    return s.bound;
+}
+
+__device__ __forceinline__ void put(uint64_t key, TopScratch &s, uint64_t *list, int listed)
+{
+    const uint32_t at = atomicAdd(&s.count, 1u);
+    if (at < (uint32_t)listed) list[at] = key;
+}
+
+// The k largest of the list's `count` entries, in order, to s.best
+__device__ __forceinline__ void best_of_list(uint32_t count, int k, TopScratch &s, const uint64_t *list)
+{
+    for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
+        const uint64_t key = list[i];
+        uint32_t ahead = 0;
+        for (uint32_t j = 0; j < count; ++j) ahead += list[j] > key;
+        if (ahead < (uint32_t)k) s.best[ahead] = key;
+    }
+    __syncthreads();
+}
+
+// The same from what `every(look)` shows of the thread's keys, one sweep for each
+template <typename Every>
+__device__ __forceinline__ void one_by_one(int k, TopScratch &s, const Every &every)
+{
+    uint64_t last = ~0ull;
+    for (int n = 0; n < k; ++n) {
+        uint64_t best = 0;
+        every([&](uint64_t key) { if (key < last && key > best) best = key; });
+        last = over_block(best, s.part, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+        if (threadIdx.x == 0) s.best[n] = last;
+        __syncthreads();
+    }
+}
+
+// what becomes of a row once its sums are known; s.best: its largest logits
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogitArgs &a, uint64_t i, const T *row, const LogPart &p, const TopScratch &s)
+{
+    const bool bad = p.r != p.r, none = p.r == -INFINITY;
+    const double log_s = log(p.s);
+    const auto log_prob = [&](T l) { return bad ? NAN : none ? -INFINITY : (float)(value_of(l, a.fl) - p.r - log_s); };
+    if (threadIdx.x == 0) {
+        if (a.lse) a.lse[i] = bad ? NAN : none ? -INFINITY : (float)(p.r + log_s);
+        if (a.entropy) a.entropy[i] = bad ? NAN : none ? 0.0f : (float)(log_s - p.e / p.s);
+        if (a.logp) {
+            const int64_t label = a.labels[i];
+            a.logp[i] = label < 0 ? 0.0f : (uint64_t)label >= a.classes ? NAN : log_prob(row[label]);
+        }
+    }
+    if ((int)threadIdx.x < a.topk) {
+        const uint32_t j = 0x7fffffffu - (uint32_t)s.best[threadIdx.x];
+        a.top_index[i * a.topk + threadIdx.x] = (int32_t)j;
+        a.top_logp[i * a.topk + threadIdx.x] = log_prob(row[j]);
+    }
+}
+
+// moves the sums of a thread or chunk to another reference
+__device__ __forceinline__ void rebase(LogPart &p, double r)
+{
+    if (p.r == -INFINITY) { p.s = p.e = 0.0; }
+    else {
+        const double k = exp(p.r - r);
+        p.e = k * (p.e + (p.r - r) * p.s);
+        p.s *= k;
+    }
+    p.r = r;
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs a, const LogChunkArgs c)
+{
+    constexpr int U = kUnit<T>, W = kWords<T>;
+    constexpr bool kFloat = __is_same(T, float);
+    typedef typename RowValue<T>::type V;
+    extern __shared__ uint64_t list[];
+    __shared__ TopScratch top;
+    __shared__ double part_r[kMostThreads / kWave], part_s[kMostThreads / kWave], part_e[kMostThreads / kWave];
+    const uint64_t i = blockIdx.x / c.splits;
+    const uint32_t chunk = blockIdx.x - (uint32_t)i * c.splits;
+    const T *row = static_cast<const T *>(a.logits) + i * a.ld;
+    // units start at 16-byte addresses
+    const uint32_t head = (uint32_t)min((uint64_t)((-(uintptr_t)row & 15) / sizeof(T)), a.classes);
+    const uint64_t whole = (a.classes - head) / U, first = min((uint64_t)chunk * c.units, whole);
+    const uint32_t units = (uint32_t)min(whole - first, (uint64_t)c.units), tail = (uint32_t)(a.classes - head - whole * U);
+    const T *body = row + head + first * U;
+    const bool on_edge = chunk == 0 && threadIdx.x < head + tail;
+    const uint32_t edge_col = threadIdx.x < head ? threadIdx.x : (uint32_t)a.classes - (head + tail) + threadIdx.x;
+
+    const float to_log2 = 1.44269504f * ldexpf(1.0f, -a.fl);
+    V r = c.fixed ? (V)0 : kFloat ? (V)-INFINITY : (V)INT32_MIN;
+    bool begun = c.fixed;
+    double s = 0.0, e = 0.0;
+    int bad = 0;
+    // a reference for values up to `largest`; false: nothing to add
+    const auto refer = [&](V largest) -> bool {
+        if (kFloat && !(largest < (V)INFINITY)) { bad = 1; return false; }
+        if (c.fixed) return true;
+        const float ahead = begun ? (float)((double)largest - (double)r) * to_log2 : INFINITY;
+        if (ahead > 11.5f && (!kFloat || largest > (V)-INFINITY)) {
+            const double d = ((double)r - (double)largest) * (double)to_log2, k = begun ? exp2(d) : 0.0;
+            e = begun ? k * (e + d * s) : 0.0;
+            s *= k;
+            r = largest;
+            begun = true;
+        }
+        return begun;
+    };
+    const auto log2_of = [&](V x) -> float {
+        if constexpr (__is_same(T, int32_t)) return (float)((double)x - (double)r) * to_log2;
+        else if constexpr (kFloat) return fmaxf((x - r) * to_log2, -200.0f);
+        else return (x - r) * to_log2;
+    };
+    // the thread's largest unit, of equal ones the first: number 0 are the head's elements, the tail's come last
+    V largest = 0;
+    uint32_t where = ~0u;
+    const uint32_t edge_unit = threadIdx.x < head ? 0 : 0x7ffffff0u;
+    const auto clean = [](V v) -> V { return v != v ? (V)-INFINITY : v; };      // fp32 only
+    V edge = 0;
+    if (on_edge) {
+        edge = (V)row[edge_col];
+        if (refer(edge)) { const float g = log2_of(edge), t = __builtin_amdgcn_exp2f(g); s += t; e += (double)(t * g); }
+        if (kFloat) edge = clean(edge);
+    }
+    for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+        uint32_t w[W];
+        load_unit(body + (uint64_t)u * U, w);
+        V v[U], m;
+#pragma unroll
+        for (int j = 0; j < U; ++j) v[j] = (V)unit_get<T>(w, j);
+        if (TOP || !c.fixed) {
+            m = v[0];
+#pragma unroll
+            for (int j = 1; j < U; ++j) {
+                if constexpr (kFloat) m = __builtin_elementwise_maximum(m, v[j]);
+                else m = m > v[j] ? m : v[j];
+            }
+        }
+        if (c.fixed || refer(m)) {
+            float us = 0.0f, ue = 0.0f;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const float g = c.fixed && !__is_same(T, int32_t) ? (float)v[j] * to_log2 : log2_of(v[j]), t = __builtin_amdgcn_exp2f(g);
+                us += t;
+                ue = fmaf(t, g, ue);
+            }
+            s += us;
+            e += ue;
+        }
+        if constexpr (TOP) {
+            if (kFloat && m != m) {
+                m = clean(v[0]);
+#pragma unroll
+                for (int j = 1; j < U; ++j) m = larger(m, clean(v[j]));
+            }
+            if (where == ~0u || m > largest) { largest = m; where = (uint32_t)first + u + 1; }
+        }
+    }
+    if (TOP && on_edge && (where == ~0u || (edge_unit == 0 ? edge >= largest : edge > largest))) { largest = edge; where = edge_unit; }
+    // one reference for the block
+    const auto maximum = [](double x, double y) { return fmax(x, y); };
+    const auto add = [](double x, double y) { return x + y; };
+    const double ln2 = 0.69314718055994530942;
+    LogPart p = {begun ? (double)r * ldexp(1.0, -a.fl) : -INFINITY, s, e * ln2};
+    if (!c.fixed) {
+        const double ref = over_block(p.r, part_r, maximum);
+        rebase(p, ref);
+    }
+    p.s = over_block(p.s, part_s, add);
+    p.e = over_block(p.e, part_e, add);
+    if (kFloat && __syncthreads_or(bad)) p.r = NAN;
+
+    if constexpr (TOP) {
+        const uint64_t mine = where == ~0u ? 0 : key_of(order_of(largest), where);
+        const uint64_t bound = bound_of(mine, a.topk, top, list);
+        if (mine >= bound && mine) {
+            if (on_edge && key_of(order_of(edge), edge_unit) >= bound) put(key_of(order_of(edge), edge_col), top, list, c.listed);
+            for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
+                uint32_t w[W];
+                load_unit(body + (uint64_t)u * U, w);
+#pragma unroll
+                for (int j = 0; j < U; ++j) {
+                    const uint32_t order = order_of((V)unit_get<T>(w, j));
+                    if (key_of(order, (uint32_t)first + u + 1) >= bound) put(key_of(order, head + ((uint32_t)first + u) * U + j), top, list, c.listed);
+                }
+            }
+        }
+        __syncthreads();
+        const uint32_t found = top.count;
+        if (found <= (uint32_t)c.listed) {
+            if ((int)threadIdx.x < a.topk) top.best[threadIdx.x] = 0;      // a chunk may have fewer
+            __syncthreads();
+            best_of_list(found, a.topk, top, list);
+        } else {
+            one_by_one(a.topk, top, [&](auto &&look) {
+                if (on_edge) look(key_of(order_of((V)row[edge_col]), edge_col));
+                for (uint32_t u = threadIdx.x; u < units; u += blockDim.x)
+                    for (int j = 0; j < U; ++j) look(key_of(order_of((V)body[(uint64_t)u * U + j]), head + ((uint32_t)first + u) * U + j));
+            });
+        }
+    }
+    if (c.splits == 1) {
+        finish_row(a, i, row, p, top);
+        return;
+    }
+    if (threadIdx.x == 0) c.part[blockIdx.x] = p;
+    if (TOP && (int)threadIdx.x < a.topk) c.keys[(uint64_t)blockIdx.x * a.topk + threadIdx.x] = top.best[threadIdx.x];
+}
+
+constexpr int kJoinThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const LogitArgs a, const LogChunkArgs c)
+{
+    extern __shared__ uint64_t list[];
+    __shared__ TopScratch top;
+    __shared__ double part_r[kMostThreads / kWave], part_s[kMostThreads / kWave], part_e[kMostThreads / kWave];
+    const uint64_t i = blockIdx.x;
+    const LogPart *parts = c.part + i * c.splits;
+    double ref = -INFINITY;
+    int bad = 0;
+    for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) {
+        ref = fmax(ref, parts[j].r);
+        bad |= parts[j].r != parts[j].r;
+    }
+    ref = over_block(ref, part_r, [](double x, double y) { return fmax(x, y); });
+    LogPart p = {ref, 0.0, 0.0};
+    for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) {
+        LogPart q = parts[j];
+        rebase(q, ref);
+        p.s += q.s;
+        p.e += q.e;
+    }
+    const auto add = [](double x, double y) { return x + y; };
+    p.s = over_block(p.s, part_s, add);
+    p.e = over_block(p.e, part_e, add);
+    if (__syncthreads_or(bad)) p.r = NAN;
+    if (a.topk > 0) {
+        const uint64_t *keys = c.keys + i * c.splits * a.topk;
+        const uint32_t n = c.splits * a.topk;
+        uint64_t mine = 0;
+        for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads) mine = keys[j] > mine ? keys[j] : mine;
+        const uint64_t bound = bound_of(mine, a.topk, top, list);
+        if (mine >= bound)
+            for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads)
+                if (keys[j] >= bound && keys[j]) put(keys[j], top, list, c.listed);
+        __syncthreads();
+        if (top.count <= (uint32_t)c.listed) {
+            best_of_list(top.count, a.topk, top, list);
+        } else {
+            one_by_one(a.topk, top, [&](auto &&look) { for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads) look(keys[j]); });
+        }
+    }
+    finish_row(a, i, static_cast<const T *>(a.logits) + i * a.ld, p, top);
+}
+
+struct LogProbsPlan {
+    uint32_t splits, units, threads;
+    size_t part_bytes, ws_bytes;
+};
+
+static LogProbsPlan plan_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, adapt_fmt f)
+{
+    const int U = f.wl != ADAPT_WL_FP32 && f.wl <= 8 ? 16 : 8;
+    LogProbsPlan p = {};
+    const uint64_t all = std::max<uint64_t>(classes / U, 1);
+    uint64_t splits = 1;
+    const uint64_t wanted = 4 * (uint64_t)num_cu;             // blocks
+    if (rows < wanted / 2 && all >= 512) splits = std::min<uint64_t>((wanted + rows - 1) / std::max<uint64_t>(rows, 1), all / 256);
+    p.units = (uint32_t)((all + splits - 1) / splits);
+    p.splits = (uint32_t)((all + p.units - 1) / p.units);
+    const uint64_t per = rows * splits >= wanted ? 8 : 2, threads = (p.units + per - 1) / per;
+    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, 512);
+    if (p.splits > 1) {
+        p.part_bytes = (rows * p.splits * sizeof(LogPart) + 255) & ~(size_t)255;
+        p.ws_bytes = p.part_bytes + rows * p.splits * topk * sizeof(uint64_t);
+    }
+    return p;
+}
+
+size_t ws_need_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, adapt_fmt f)
+{
+    return plan_log_probs(num_cu, rows, classes, topk, f).ws_bytes + 16;
+}
 
 // How the rows of a cross entropy are cut: rows too few to fill the card into chunks, whose sums are a launch of their own.
 struct CrossEntropyPlan {
@@ -423,6 +671,22 @@ using namespace adapt;
 
 static int logit_bytes(adapt_fmt f) { return f.wl == ADAPT_WL_FP32 ? 4 : storage_bytes(f); }
 
+template <typename T>
+static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsPlan &p, int wl)
+{
+    const int span = sizeof(T) == 4 ? wl : 8 * (int)sizeof(T);
+    const bool fixed = !__is_same(T, float) && span - 1 - a.fl <= 4;
+    LogChunkArgs c = {p.splits, p.units, reinterpret_cast<LogPart *>(scratch(ctx)), reinterpret_cast<uint64_t *>(scratch(ctx) + p.part_bytes),
+                      (int)(4 * p.threads), fixed};
+    const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
+    if (a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true>), grid, block, c.listed * sizeof(uint64_t), ctx->stream, a, c);
+    else hipLaunchKernelGGL((log_probs_kernel<T, false>), grid, block, 0, ctx->stream, a, c);
+    if (p.splits > 1) {
+        c.listed = 1024;
+        hipLaunchKernelGGL(join_log_probs_kernel<T>, dim3((unsigned)a.rows), dim3(kJoinThreads), a.topk ? c.listed * sizeof(uint64_t) : 0, ctx->stream, a, c);
+    }
+}
+
 extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes, size_t ld, const int64_t *labels,
                                float *logp, float *lse, float *entropy, int topk, int32_t *top_index, float *top_logp)
 {
@@ -439,11 +703,13 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     a.fl = f.wl == ADAPT_WL_FP32 ? 0 : f.fl;
     a.labels = labels; a.logp = logp; a.lse = lse; a.entropy = entropy;
     a.topk = topk; a.top_index = top_index; a.top_logp = top_logp;
-    const dim3 grid((unsigned)std::min<size_t>(rows, 1u << 20)), block(kRowThreads);
-    if (f.wl == ADAPT_WL_FP32) hipLaunchKernelGGL(log_probs_kernel<float>, grid, block, 0, ctx->stream, a);
-    else if (f.wl <= 8) hipLaunchKernelGGL(log_probs_kernel<int8_t>, grid, block, 0, ctx->stream, a);
-    else if (f.wl <= 16) hipLaunchKernelGGL(log_probs_kernel<int16_t>, grid, block, 0, ctx->stream, a);
-    else hipLaunchKernelGGL(log_probs_kernel<int32_t>, grid, block, 0, ctx->stream, a);
+    const LogProbsPlan p = plan_log_probs(ctx->num_cu, rows, classes, topk, f);
+    if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
+    if (rows * p.splits >= (1ull << 31)) return ADAPT_EUNSUPPORTED;
+    if (f.wl == ADAPT_WL_FP32) launch_log_probs<float>(ctx, a, p, f.wl);
+    else if (f.wl <= 8) launch_log_probs<int8_t>(ctx, a, p, f.wl);
+    else if (f.wl <= 16) launch_log_probs<int16_t>(ctx, a, p, f.wl);
+    else launch_log_probs<int32_t>(ctx, a, p, f.wl);
     return hip_status(ctx, hipGetLastError());
 }
 
