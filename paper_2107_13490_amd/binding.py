@@ -303,15 +303,6 @@ def _fmt(f):
 _FP32 = Fmt(0, 0)      # fp32 logits
 
 
-def _dense_rows(t):
-    """A matrix whose rows are dense and do not overlap."""
-    return t.numel() == 0 or ((t.shape[1] == 1 or t.stride(1) == 1) and (t.shape[0] == 1 or t.stride(0) >= t.shape[1]))
-
-
-def _row_stride(t):
-    return t.stride(0) if t.shape[0] > 1 and t.shape[1] > 0 else t.shape[1]
-
-
 # Descriptor arrays of the batched calls: the values of all items in order, packed at once.  Building one ctypes structure per item
 # costs more host time than the call (a window of 25 gradients 17 us, packed 7).  What does not pack (a negative stream, a word
 # length that is no integer or longer than its field) goes into the structures, which wrap or refuse it.
@@ -731,17 +722,32 @@ class Context:
         return out, shift, e_out
 
     # -- dropout, log probabilities, cross entropy --------------------------------------------------
-    def _own(self, what, t, shape=None, dtype=None, rows=False):
-        """Checks a tensor of the calls below: on the context's device, of the given shape and type, dense (rows: with
-        dense rows)."""
-        if not t.is_cuda or t.device.index != self._device:
+    def _own(self, what, t, dtype, shape=None):
+        """Checks a tensor of the calls below: on the context's device, of the given type and shape, dense (a matrix without
+        a given shape: with dense rows)."""
+        if t.get_device() != self._device:
             raise ValueError(f"{what} is on {t.device}, the context on cuda:{self._device}")
-        if dtype is not None and t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{what} is {t.dtype}, not {dtype}")
         if shape is not None and t.shape != shape:
             raise ValueError(f"{what} has the shape {tuple(t.shape)}, not {tuple(shape)}")
-        if not (_dense_rows(t) if rows else t.is_contiguous()):
-            raise ValueError(f"{what} has strides {t.stride()} that the call does not take")
+        if not t.is_contiguous():
+            raise ValueError(f"{what} has strides {t.stride()}: the call takes dense tensors")
+
+    def _matrix(self, what, t, dtype):
+        """The same for a matrix whose rows may lie further apart than they are long; returns (rows, columns, row stride)."""
+        if t.dim() != 2:
+            raise ValueError(f"{what} has the shape {tuple(t.shape)}: rows x classes are wanted")
+        if t.is_contiguous():
+            self._own(what, t, dtype)
+            rows, cols = t.shape
+            return rows, cols, cols
+        self._own(what, t[:0], dtype)
+        rows, cols = t.shape
+        apart = t.stride(0) if rows > 1 else cols
+        if apart < cols or (cols > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} has strides {t.stride()}: the call takes rows that are dense and do not overlap")
+        return rows, cols, apart
 
     def dropout(self, x, fx, p, fo=None, res=None, fres=None, mode=SR, seed=0, stream=0, out=None):
         """Codes of format fx = (wl, fl) dropped with probability p and scaled by its counterpart, as codes of format fo
@@ -749,28 +755,31 @@ class Context:
         the same p, seed and stream; mode is the rounding of the kept ones."""
         fx = _fmt(fx)
         fo = fx if fo is None else _fmt(fo)
-        self._own("x", x, dtype=self.storage_dtype(fx.wl))
+        codes = self._codes
+        self._own("x", x, codes(fx.wl))
         if res is None:
             fres = fx
         else:
             fres = _fmt(fres)
-            self._own("res", res, x.shape, self.storage_dtype(fres.wl))
+            self._own("res", res, codes(fres.wl), x.shape)
         if out is None:
-            out = self._torch.empty(x.shape, dtype=self.storage_dtype(fo.wl), device=x.device)
+            out = self._torch.empty(x.shape, dtype=codes(fo.wl), device=x.device)
         else:
-            self._own("out", out, x.shape, self.storage_dtype(fo.wl))
-        _check(self._lib.adapt_dropout(self._h, _ptr(x), fx, x.numel(), p, fo, Rng(mode, seed, stream), _ptr(res), fres, _ptr(out)),
-               "adapt_dropout")
+            self._own("out", out, codes(fo.wl), x.shape)
+        _check(self._lib.adapt_dropout(self._h, x.data_ptr(), fx, x.numel(), p, fo, Rng(mode, seed, stream), _ptr(res), fres,
+                                       out.data_ptr()), "adapt_dropout")
         return out
+
+    def _codes(self, wl):
+        torch = self._torch
+        return torch.int8 if wl <= 8 else torch.int16 if wl <= 16 else torch.int32
 
     def _logits(self, logits, f):
         """(format, rows, classes, row stride) of a matrix of logits: codes of format f, or fp32 (f = None)."""
-        f = _FP32 if f is None else _fmt(f)
-        if logits.dim() != 2:
-            raise ValueError(f"logits have the shape {tuple(logits.shape)}: rows x classes are wanted")
-        self._own("logits", logits, dtype=self.storage_dtype(f.wl) if f.wl else self._torch.float32, rows=True)
-        rows, classes = logits.shape
-        return f, rows, classes, _row_stride(logits)
+        if f is None:
+            return _FP32, *self._matrix("logits", logits, self._torch.float32)
+        f = _fmt(f)
+        return f, *self._matrix("logits", logits, self._codes(f.wl))
 
     def log_probs(self, logits, f, labels=None, topk=0, entropy=True):
         """logits: rows x classes codes of format f = (wl, fl), or fp32 (f = None); a row may be longer than its classes
@@ -779,7 +788,7 @@ class Context:
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
         if labels is not None:
-            self._own("labels", labels, (rows,), torch.int64)
+            self._own("labels", labels, torch.int64, (rows,))
         dev = logits.device
         lse = torch.empty(rows, dtype=torch.float32, device=dev)
         logp = torch.empty(rows, dtype=torch.float32, device=dev) if labels is not None else None
@@ -797,16 +806,19 @@ class Context:
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
         fg = _fmt(fg)
-        self._own("labels", labels, (rows,), torch.int64)
+        self._own("labels", labels, torch.int64, (rows,))
         if weights is not None:
-            self._own("weights", weights, (rows,), torch.float32)
+            self._own("weights", weights, torch.float32, (rows,))
+        ldg = classes
         if out is None:
-            out = torch.empty((rows, classes), dtype=self.storage_dtype(fg.wl), device=logits.device)
+            out = torch.empty((rows, classes), dtype=self._codes(fg.wl), device=logits.device)
         else:
-            self._own("out", out, logits.shape, self.storage_dtype(fg.wl), rows=True)
+            if out.shape != logits.shape:
+                raise ValueError(f"out has the shape {tuple(out.shape)}, not {tuple(logits.shape)}")
+            ldg = self._matrix("out", out, self._codes(fg.wl))[2]
         logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
         _check(self._lib.adapt_cross_entropy(self._h, _ptr(logits), f, rows, classes, ld, _ptr(labels), _ptr(weights), fg,
-                                             Rng(mode, seed, stream), _ptr(out), _row_stride(out), _ptr(logp)), "adapt_cross_entropy")
+                                             Rng(mode, seed, stream), _ptr(out), ldg, _ptr(logp)), "adapt_cross_entropy")
         return out, logp
 
 

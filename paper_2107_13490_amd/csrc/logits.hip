@@ -113,17 +113,60 @@ template <> __device__ __forceinline__ float lowest<float>() { return -INFINITY;
 template <typename T> __device__ __forceinline__ T larger(T a, T b) { return a > b ? a : b; }
 template <> __device__ __forceinline__ float larger<float>(float a, float b) { return fmaxf(a, b); }
 
-// reduction over the block; `part` is used once
+// the value of the lane N places on in its row of 16
+template <int N, typename V>
+__device__ __forceinline__ V from_row(V v)
+{
+    constexpr int kWordsOf = (sizeof(V) + 3) / 4;
+    uint32_t w[kWordsOf] = {};
+    __builtin_memcpy(w, &v, sizeof(V));
+#pragma unroll
+    for (int k = 0; k < kWordsOf; ++k) w[k] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[k], 0x120 + N, 0xf, 0xf, false);
+    __builtin_memcpy(&v, w, sizeof(V));
+    return v;
+}
+
+// reduction over a wavefront, all of whose lanes take part: in lane 0
+template <typename V, typename Op>
+__device__ __forceinline__ V over_wave(V v, Op op)
+{
+    v = op(v, from_row<8>(v));
+    v = op(v, from_row<4>(v));
+    v = op(v, from_row<2>(v));
+    v = op(v, from_row<1>(v));
+    v = op(v, (V)__shfl_xor(v, 16, 64));
+    return op(v, (V)__shfl_xor(v, 32, 64));
+}
+
+// reduction over the block, in every thread; `part` is used once
 template <typename V, typename Op>
 __device__ __forceinline__ V over_block(V v, V *part, Op op)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = op(v, (V)__shfl_xor(v, off, 64));
+    v = over_wave(v, op);
     if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
     v = part[0];
     for (int w = 1; w < (int)(blockDim.x / kWave); ++w) v = op(v, part[w]);
     return v;
+}
+
+struct Pair { double a, b; };
+__device__ __forceinline__ Pair sums_over_block(Pair v, Pair *part)
+{
+    const auto add = [](double x, double y) { return x + y; };
+    v.a = over_wave(v.a, add);
+    v.b = over_wave(v.b, add);
+    if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+    for (int w = 1; w < (int)(blockDim.x / kWave); ++w) { v.a += part[w].a; v.b += part[w].b; }
+    return v;
+}
+
+// a 64-bit value of one lane, in all
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 
 struct RowPart { double m, s; };      // largest value (0: not needed) and sum of a chunk
@@ -309,7 +352,6 @@ struct LogChunkArgs {
     LogPart *part;                       // [row][chunk]
     uint64_t *keys;                      // [row][chunk][topk]
     int listed;                          // entries of the list
-    bool fixed;                          // r = 0
 };
 
 template <typename T> struct RowValue { typedef float type; };      // 8- and 16-bit codes are exact in fp32
@@ -318,20 +360,21 @@ template <> struct RowValue<int32_t> { typedef int type; };
 // scratch of the selection, in LDS
 struct TopScratch {
     uint64_t bound;
-    uint32_t count;
+    uint32_t count, reaching;
     uint32_t ahead[kWave];      // groups ahead of this one, and (16 bits up) those not behind it
     uint64_t group[kWave];
     uint64_t best[kMaxTop];
     uint64_t part[kMostThreads / kWave];
+    uint16_t reach[kMostThreads];
 };
 
-// The bound for the k largest from one key per thread (0: none); scratch.count = 0 afterwards
+// The bound for the k largest from one key per thread (0: none); the scratch's counts are 0 afterwards
 __device__ __forceinline__ uint64_t bound_of(uint64_t key, int k, TopScratch &s, uint64_t *list)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
     list[threadIdx.x] = key;
     if (threadIdx.x < kWave) s.ahead[lane] = 0;
-    if (threadIdx.x == 0) { s.bound = 0; s.count = 0; }
+    if (threadIdx.x == 0) { s.bound = 0; s.count = s.reaching = 0; }
     __syncthreads();
     if (wave == 0) {
         for (int w = 1; w < waves; ++w) { const uint64_t o = list[w * kWave + lane]; key = o > key ? o : key; }
@@ -340,7 +383,10 @@ __device__ __forceinline__ uint64_t bound_of(uint64_t key, int k, TopScratch &s,
     __syncthreads();
     key = s.group[lane];
     uint32_t ahead = 0;
-    for (int j = wave; j < kWave; j += waves) ahead += (s.group[j] > key ? 0x10001u : 0u) + (s.group[j] == key ? 0x10000u : 0u);
+    for (int j = wave; j < kWave; j += waves) {
+        const uint64_t other = of_lane(key, __builtin_amdgcn_readfirstlane(j));
+        ahead += other > key ? 0x10001u : other == key ? 0x10000u : 0u;
+    }
     atomicAdd(&s.ahead[lane], ahead);
     __syncthreads();
     ahead = s.ahead[lane];
@@ -356,13 +402,24 @@ __device__ __forceinline__ void put(uint64_t key, TopScratch &s, uint64_t *list,
 }
 
 // The k largest of the list's `count` entries, in order, to s.best
-__device__ __forceinline__ void best_of_list(uint32_t count, int k, TopScratch &s, const uint64_t *list)
+__device__ __forceinline__ void best_of_list(const uint32_t found, int k, TopScratch &s, const uint64_t *list)
 {
-    for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
-        const uint64_t key = list[i];
-        uint32_t ahead = 0;
-        for (uint32_t j = 0; j < count; ++j) ahead += list[j] > key;
-        if (ahead < (uint32_t)k) s.best[ahead] = key;
+    const uint32_t count = __builtin_amdgcn_readfirstlane(found);      // the same in every thread
+    if (count <= (uint32_t)kWave) {
+        if (threadIdx.x < kWave) {
+            const uint64_t key = threadIdx.x < count ? list[threadIdx.x] : 0;
+            int ahead = 0;
+            for (uint32_t j = 0; j < count; ++j) ahead += of_lane(key, (int)j) > key;
+            if (threadIdx.x < count && ahead < k) s.best[ahead] = key;
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
+            const uint64_t key = list[i];
+            uint32_t ahead = 0;
+#pragma unroll 8
+            for (uint32_t j = 0; j < count; ++j) ahead += list[j] > key;
+            if (ahead < (uint32_t)k) s.best[ahead] = key;
+        }
     }
     __syncthreads();
 }
@@ -381,25 +438,49 @@ __device__ __forceinline__ void one_by_one(int k, TopScratch &s, const Every &ev
     }
 }
 
-// what becomes of a row once its sums are known; s.best: its largest logits
+// log of a positive number, good to 2^-23 (absolutely, where the result is below 1): the fp32 logarithm of its mantissa
+__device__ __forceinline__ double log_of_sum(double s)
+{
+    int k;
+    const float m = (float)frexp(s, &k);
+    return fma((double)k, 0.69314718055994530942, (double)logf(m));
+}
+
+// a row's label and its logit, loaded before they are needed
 template <typename T>
-__device__ __forceinline__ void finish_row(const LogitArgs &a, uint64_t i, const T *row, const LogPart &p, const TopScratch &s)
+struct LabelOf {
+    int64_t label = -1;
+    T logit = 0;
+    __device__ __forceinline__ LabelOf(const LogitArgs &a, uint64_t i, const T *row)
+    {
+        if (a.logp) label = a.labels[i];
+        if (label >= 0 && (uint64_t)label < a.classes) logit = row[label];
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ double value_of_order(uint32_t order, int fl)
+{
+    if constexpr (__is_same(T, float)) return (double)__uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order);
+    else if constexpr (sizeof(T) == 4) return value_of((int32_t)(order ^ 0x80000000u), fl);
+    else return ldexp((double)__uint_as_float((order & 0x80000000u) ? order & 0x7fffffffu : ~order), -fl);
+}
+
+// what becomes of a row once its sums are known, for threads 0.. of a row; `best`: the thread's share of its largest logits
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogitArgs &a, uint64_t i, const LabelOf<T> &l, const LogPart &p, int thread, uint64_t best)
 {
     const bool bad = p.r != p.r, none = p.r == -INFINITY;
-    const double log_s = log(p.s);
-    const auto log_prob = [&](T l) { return bad ? NAN : none ? -INFINITY : (float)(value_of(l, a.fl) - p.r - log_s); };
-    if (threadIdx.x == 0) {
+    const double log_s = log_of_sum(p.s);
+    const auto log_prob = [&](double x) { return bad ? NAN : none ? -INFINITY : (float)(x - p.r - log_s); };
+    if (thread == 0) {
         if (a.lse) a.lse[i] = bad ? NAN : none ? -INFINITY : (float)(p.r + log_s);
         if (a.entropy) a.entropy[i] = bad ? NAN : none ? 0.0f : (float)(log_s - p.e / p.s);
-        if (a.logp) {
-            const int64_t label = a.labels[i];
-            a.logp[i] = label < 0 ? 0.0f : (uint64_t)label >= a.classes ? NAN : log_prob(row[label]);
-        }
+        if (a.logp) a.logp[i] = l.label < 0 ? 0.0f : (uint64_t)l.label >= a.classes ? NAN : log_prob(value_of(l.logit, a.fl));
     }
-    if ((int)threadIdx.x < a.topk) {
-        const uint32_t j = 0x7fffffffu - (uint32_t)s.best[threadIdx.x];
-        a.top_index[i * a.topk + threadIdx.x] = (int32_t)j;
-        a.top_logp[i * a.topk + threadIdx.x] = log_prob(row[j]);
+    if (thread < a.topk) {
+        a.top_index[i * a.topk + thread] = (int32_t)(0x7fffffffu - (uint32_t)best);
+        a.top_logp[i * a.topk + thread] = log_prob(value_of_order<T>((uint32_t)(best >> 32), a.fl));
     }
 }
 
@@ -415,7 +496,7 @@ __device__ __forceinline__ void rebase(LogPart &p, double r)
     p.r = r;
 }
 
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool FIXED>
 __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs a, const LogChunkArgs c)
 {
     constexpr int U = kUnit<T>, W = kWords<T>;
@@ -423,7 +504,8 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
     typedef typename RowValue<T>::type V;
     extern __shared__ uint64_t list[];
     __shared__ TopScratch top;
-    __shared__ double part_r[kMostThreads / kWave], part_s[kMostThreads / kWave], part_e[kMostThreads / kWave];
+    __shared__ double part_r[kMostThreads / kWave];
+    __shared__ Pair part_s[kMostThreads / kWave];
     const uint64_t i = blockIdx.x / c.splits;
     const uint32_t chunk = blockIdx.x - (uint32_t)i * c.splits;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
@@ -435,15 +517,16 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
     const bool on_edge = chunk == 0 && threadIdx.x < head + tail;
     const uint32_t edge_col = threadIdx.x < head ? threadIdx.x : (uint32_t)a.classes - (head + tail) + threadIdx.x;
 
+    const LabelOf<T> wanted(a, i, row);
     const float to_log2 = 1.44269504f * ldexpf(1.0f, -a.fl);
-    V r = c.fixed ? (V)0 : kFloat ? (V)-INFINITY : (V)INT32_MIN;
-    bool begun = c.fixed;
+    V r = FIXED ? (V)0 : kFloat ? (V)-INFINITY : (V)INT32_MIN;
+    bool begun = FIXED;
     double s = 0.0, e = 0.0;
     int bad = 0;
     // a reference for values up to `largest`; false: nothing to add
     const auto refer = [&](V largest) -> bool {
         if (kFloat && !(largest < (V)INFINITY)) { bad = 1; return false; }
-        if (c.fixed) return true;
+        if (FIXED) return true;
         const float ahead = begun ? (float)((double)largest - (double)r) * to_log2 : INFINITY;
         if (ahead > 11.5f && (!kFloat || largest > (V)-INFINITY)) {
             const double d = ((double)r - (double)largest) * (double)to_log2, k = begun ? exp2(d) : 0.0;
@@ -455,7 +538,8 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
         return begun;
     };
     const auto log2_of = [&](V x) -> float {
-        if constexpr (__is_same(T, int32_t)) return (float)((double)x - (double)r) * to_log2;
+        if constexpr (FIXED) return (float)x * to_log2;
+        else if constexpr (__is_same(T, int32_t)) return (float)((double)x - (double)r) * to_log2;
         else if constexpr (kFloat) return fmaxf((x - r) * to_log2, -200.0f);
         else return (x - r) * to_log2;
     };
@@ -476,19 +560,20 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
         V v[U], m;
 #pragma unroll
         for (int j = 0; j < U; ++j) v[j] = (V)unit_get<T>(w, j);
-        if (TOP || !c.fixed) {
+        if (TOP || !FIXED) {
             m = v[0];
 #pragma unroll
             for (int j = 1; j < U; ++j) {
                 if constexpr (kFloat) m = __builtin_elementwise_maximum(m, v[j]);
-                else m = m > v[j] ? m : v[j];
+                else if constexpr (sizeof(T) < 4) m = __builtin_elementwise_maximum(m, v[j]);
+                else m = max(m, v[j]);
             }
         }
-        if (c.fixed || refer(m)) {
+        if (FIXED || refer(m)) {
             float us = 0.0f, ue = 0.0f;
 #pragma unroll
             for (int j = 0; j < U; ++j) {
-                const float g = c.fixed && !__is_same(T, int32_t) ? (float)v[j] * to_log2 : log2_of(v[j]), t = __builtin_amdgcn_exp2f(g);
+                const float g = log2_of(v[j]), t = __builtin_amdgcn_exp2f(g);
                 us += t;
                 ue = fmaf(t, g, ue);
             }
@@ -507,30 +592,34 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
     if (TOP && on_edge && (where == ~0u || (edge_unit == 0 ? edge >= largest : edge > largest))) { largest = edge; where = edge_unit; }
     // one reference for the block
     const auto maximum = [](double x, double y) { return fmax(x, y); };
-    const auto add = [](double x, double y) { return x + y; };
     const double ln2 = 0.69314718055994530942;
     LogPart p = {begun ? (double)r * ldexp(1.0, -a.fl) : -INFINITY, s, e * ln2};
-    if (!c.fixed) {
+    if (!FIXED) {
         const double ref = over_block(p.r, part_r, maximum);
         rebase(p, ref);
     }
-    p.s = over_block(p.s, part_s, add);
-    p.e = over_block(p.e, part_e, add);
+    const Pair sums = sums_over_block({p.s, p.e}, part_s);
+    p.s = sums.a;
+    p.e = sums.b;
     if (kFloat && __syncthreads_or(bad)) p.r = NAN;
 
     if constexpr (TOP) {
         const uint64_t mine = where == ~0u ? 0 : key_of(order_of(largest), where);
         const uint64_t bound = bound_of(mine, a.topk, top, list);
-        if (mine >= bound && mine) {
-            if (on_edge && key_of(order_of(edge), edge_unit) >= bound) put(key_of(order_of(edge), edge_col), top, list, c.listed);
-            for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
-                uint32_t w[W];
-                load_unit(body + (uint64_t)u * U, w);
+        // the threads that reach it, then their units, spread over all threads
+        if (mine >= bound && mine) top.reach[atomicAdd(&top.reaching, 1u)] = (uint16_t)threadIdx.x;
+        if (on_edge && key_of(order_of(edge), edge_unit) >= bound) put(key_of(order_of(edge), edge_col), top, list, c.listed);
+        __syncthreads();
+        const uint32_t each = (units + blockDim.x - 1) / blockDim.x, pairs = top.reaching * each;
+        for (uint32_t n = threadIdx.x; n < pairs; n += blockDim.x) {
+            const uint32_t thread = n / each, u = top.reach[thread] + (n - thread * each) * blockDim.x;
+            if (u >= units) continue;
+            uint32_t w[W];
+            load_unit(body + (uint64_t)u * U, w);
 #pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    const uint32_t order = order_of((V)unit_get<T>(w, j));
-                    if (key_of(order, (uint32_t)first + u + 1) >= bound) put(key_of(order, head + ((uint32_t)first + u) * U + j), top, list, c.listed);
-                }
+            for (int j = 0; j < U; ++j) {
+                const uint32_t order = order_of((V)unit_get<T>(w, j));
+                if (key_of(order, (uint32_t)first + u + 1) >= bound) put(key_of(order, head + ((uint32_t)first + u) * U + j), top, list, c.listed);
             }
         }
         __syncthreads();
@@ -548,11 +637,114 @@ __global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs
         }
     }
     if (c.splits == 1) {
-        finish_row(a, i, row, p, top);
+        finish_row(a, i, wanted, p, threadIdx.x, (int)threadIdx.x < a.topk ? top.best[threadIdx.x] : 0);
         return;
     }
     if (threadIdx.x == 0) c.part[blockIdx.x] = p;
     if (TOP && (int)threadIdx.x < a.topk) c.keys[(uint64_t)blockIdx.x * a.topk + threadIdx.x] = top.best[threadIdx.x];
+}
+
+// Rows of up to kSmall classes: a wavefront each, whose lanes hold their logits
+constexpr int kSmall = 256, kSmallThreads = 256;
+
+template <typename T>
+struct SmallRow {
+    static constexpr int N = kSmall / kWave;
+    T l[N];
+    double m;          // largest; -inf: no class possible; NaN: not a distribution
+    __device__ __forceinline__ SmallRow(const T *row, int classes, int fl)
+    {
+        const int lane = threadIdx.x & (kWave - 1);
+        int bad = 0;
+        m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            l[k] = lane + k * kWave < classes ? row[lane + k * kWave] : lowest<T>();
+            if (lane + k * kWave < classes) {
+                if (__is_same(T, float)) bad |= !(l[k] < (T)INFINITY);
+                m = fmax(m, value_of(l[k], fl));
+            }
+        }
+        m = over_wave(m, [](double x, double y) { return fmax(x, y); });
+        if (__is_same(T, float) && __ballot(bad)) m = NAN;
+    }
+};
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v = over_wave(v, [](double x, double y) { return x + y; });
+    return __longlong_as_double((long long)of_lane((uint64_t)__double_as_longlong(v), 0));      // the lanes add in different orders
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kSmallThreads) log_probs_small_kernel(const LogitArgs a)
+{
+    typedef typename RowValue<T>::type V;
+    constexpr int N = SmallRow<T>::N;
+    const uint64_t i = (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
+    if (i >= a.rows) return;
+    const int lane = threadIdx.x & (kWave - 1), classes = (int)a.classes;
+    const T *row = static_cast<const T *>(a.logits) + i * a.ld;
+    const LabelOf<T> wanted(a, i, row);
+    const SmallRow<T> x(row, classes, a.fl);
+    LogPart p = {x.m, 0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const double d = value_of(x.l[k], a.fl) - x.m;
+        if (k * kWave < classes && lane + k * kWave < classes && d > -700.0) {
+            const float t = expf((float)d);
+            p.s += t;
+            p.e += t * d;
+        }
+    }
+    p.s = wave_sum(p.s);
+    p.e = wave_sum(p.e);
+    uint64_t best = 0, last = ~0ull;
+    for (int n = 0; n < a.topk; ++n) {
+        uint64_t key = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const uint64_t o = lane + k * kWave < classes ? key_of(order_of((V)x.l[k]), lane + k * kWave) : 0;
+            if (o < last && o > key) key = o;
+        }
+        last = over_wave(key, [](uint64_t u, uint64_t v) { return u > v ? u : v; });
+        if (lane == n) best = last;
+    }
+    finish_row(a, i, wanted, p, lane, best);
+}
+
+template <typename T, typename G>
+__global__ void __launch_bounds__(kSmallThreads) cross_entropy_small_kernel(const LogitArgs a)
+{
+    constexpr int N = SmallRow<T>::N;
+    const uint64_t i = (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
+    if (i >= a.rows) return;
+    const int lane = threadIdx.x & (kWave - 1), classes = (int)a.classes;
+    const T *row = static_cast<const T *>(a.logits) + i * a.ld;
+    const int64_t label = a.labels[i];
+    const bool there = label >= 0 && (uint64_t)label < a.classes;
+    const double at_label = there ? value_of(row[label], a.fl) : 0.0, weight = a.weights ? (double)a.weights[i] : 1.0;
+    const SmallRow<T> x(row, classes, a.fl);
+    double e[N], s = 0.0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        e[k] = 0.0;
+        if (k * kWave < classes && lane + k * kWave < classes) e[k] = exp(value_of(x.l[k], a.fl) - x.m);
+        s += e[k];
+    }
+    s = wave_sum(s);
+    const bool counts = there && x.m > -INFINITY;
+    if (lane == 0 && a.logp)
+        a.logp[i] = label < 0 ? 0.0f : !there || x.m != x.m ? NAN : x.m == -INFINITY ? -INFINITY : (float)(at_label - x.m - log(s));
+    const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0, scale = weight * ldexp(1.0, a.fl_g + 16) / s;
+    G *grad = static_cast<G *>(a.grad) + i * a.ldg;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int j = lane + k * kWave;
+        if (j >= classes) break;
+        const double t = floor(fmin(fmax((j == label ? e[k] - s : e[k]) * scale, tmin), tmax));
+        const long long q = ((long long)t + rounding_bits_of(a.seed, a.stream, i * a.classes + j, a.mode)) >> 16;
+        grad[j] = counts ? (G)q : (G)0;
+    }
 }
 
 constexpr int kJoinThreads = 256;
@@ -561,8 +753,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const Logi
 {
     extern __shared__ uint64_t list[];
     __shared__ TopScratch top;
-    __shared__ double part_r[kMostThreads / kWave], part_s[kMostThreads / kWave], part_e[kMostThreads / kWave];
+    __shared__ double part_r[kMostThreads / kWave];
+    __shared__ Pair part_s[kMostThreads / kWave];
     const uint64_t i = blockIdx.x;
+    const LabelOf<T> wanted(a, i, static_cast<const T *>(a.logits) + i * a.ld);
     const LogPart *parts = c.part + i * c.splits;
     double ref = -INFINITY;
     int bad = 0;
@@ -578,27 +772,30 @@ __global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const Logi
         p.s += q.s;
         p.e += q.e;
     }
-    const auto add = [](double x, double y) { return x + y; };
-    p.s = over_block(p.s, part_s, add);
-    p.e = over_block(p.e, part_e, add);
+    const Pair sums = sums_over_block({p.s, p.e}, part_s);
+    p.s = sums.a;
+    p.e = sums.b;
     if (__syncthreads_or(bad)) p.r = NAN;
     if (a.topk > 0) {
+        // a thread's keys are those of whole chunks, each chunk's in order
         const uint64_t *keys = c.keys + i * c.splits * a.topk;
-        const uint32_t n = c.splits * a.topk;
         uint64_t mine = 0;
-        for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads) mine = keys[j] > mine ? keys[j] : mine;
+        for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) mine = max(mine, keys[(uint64_t)j * a.topk]);
         const uint64_t bound = bound_of(mine, a.topk, top, list);
-        if (mine >= bound)
-            for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads)
-                if (keys[j] >= bound && keys[j]) put(keys[j], top, list, c.listed);
+        for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads)
+            for (int n = 0; n < a.topk; ++n) {
+                const uint64_t key = keys[(uint64_t)j * a.topk + n];
+                if (key < bound || key == 0) break;
+                put(key, top, list, c.listed);
+            }
         __syncthreads();
         if (top.count <= (uint32_t)c.listed) {
             best_of_list(top.count, a.topk, top, list);
         } else {
-            one_by_one(a.topk, top, [&](auto &&look) { for (uint32_t j = threadIdx.x; j < n; j += kJoinThreads) look(keys[j]); });
+            one_by_one(a.topk, top, [&](auto &&look) { for (uint32_t j = threadIdx.x; j < c.splits * a.topk; j += kJoinThreads) look(keys[j]); });
         }
     }
-    finish_row(a, i, static_cast<const T *>(a.logits) + i * a.ld, p, top);
+    finish_row(a, i, wanted, p, threadIdx.x, (int)threadIdx.x < a.topk ? top.best[threadIdx.x] : 0);
 }
 
 struct LogProbsPlan {
@@ -677,10 +874,15 @@ static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsP
     const int span = sizeof(T) == 4 ? wl : 8 * (int)sizeof(T);
     const bool fixed = !__is_same(T, float) && span - 1 - a.fl <= 4;
     LogChunkArgs c = {p.splits, p.units, reinterpret_cast<LogPart *>(scratch(ctx)), reinterpret_cast<uint64_t *>(scratch(ctx) + p.part_bytes),
-                      (int)(4 * p.threads), fixed};
+                      (int)(4 * p.threads)};
     const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
-    if (a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true>), grid, block, c.listed * sizeof(uint64_t), ctx->stream, a, c);
-    else hipLaunchKernelGGL((log_probs_kernel<T, false>), grid, block, 0, ctx->stream, a, c);
+    const size_t lds = a.topk > 0 ? c.listed * sizeof(uint64_t) : 0;
+    if constexpr (!__is_same(T, float)) {
+        if (fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, true>), grid, block, lds, ctx->stream, a, c);
+        else if (fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, true>), grid, block, lds, ctx->stream, a, c);
+    }
+    if (!fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, false>), grid, block, lds, ctx->stream, a, c);
+    else if (!fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, false>), grid, block, lds, ctx->stream, a, c);
     if (p.splits > 1) {
         c.listed = 1024;
         hipLaunchKernelGGL(join_log_probs_kernel<T>, dim3((unsigned)a.rows), dim3(kJoinThreads), a.topk ? c.listed * sizeof(uint64_t) : 0, ctx->stream, a, c);
@@ -703,6 +905,14 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     a.fl = f.wl == ADAPT_WL_FP32 ? 0 : f.fl;
     a.labels = labels; a.logp = logp; a.lse = lse; a.entropy = entropy;
     a.topk = topk; a.top_index = top_index; a.top_logp = top_logp;
+    if (classes <= (size_t)kSmall) {
+        const dim3 grid((unsigned)((rows + kSmallThreads / kWave - 1) / (kSmallThreads / kWave))), block(kSmallThreads);
+        if (f.wl == ADAPT_WL_FP32) hipLaunchKernelGGL(log_probs_small_kernel<float>, grid, block, 0, ctx->stream, a);
+        else if (f.wl <= 8) hipLaunchKernelGGL(log_probs_small_kernel<int8_t>, grid, block, 0, ctx->stream, a);
+        else if (f.wl <= 16) hipLaunchKernelGGL(log_probs_small_kernel<int16_t>, grid, block, 0, ctx->stream, a);
+        else hipLaunchKernelGGL(log_probs_small_kernel<int32_t>, grid, block, 0, ctx->stream, a);
+        return hip_status(ctx, hipGetLastError());
+    }
     const LogProbsPlan p = plan_log_probs(ctx->num_cu, rows, classes, topk, f);
     if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
     if (rows * p.splits >= (1ull << 31)) return ADAPT_EUNSUPPORTED;
@@ -718,6 +928,11 @@ static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const Cross
 {
     // distances to the largest code: of the storage for int16 (they index tables), of the format for int32
     const int span = sizeof(T) == 2 ? 16 : wl;
+    if (a.classes <= (uint64_t)kSmall) {
+        constexpr int kRows = kSmallThreads / kWave;
+        hipLaunchKernelGGL((cross_entropy_small_kernel<T, G>), dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kSmallThreads), 0, ctx->stream, a);
+        return;
+    }
     const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), span - a.fl <= 9, (int)((1ll << (span - 1)) - 1)};
     const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
     if (p.splits == 1) {
