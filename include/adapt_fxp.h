@@ -667,6 +667,13 @@ int adapt_net_create_wide(adapt_ctx *ctx, const adapt_layer_desc *layers, int co
 int adapt_net_destroy(adapt_net *net);
 /* <WL,FL> of layer l: its weights, its output activations, and (WL only) its gradients. */
 int adapt_net_set_format(adapt_net *net, int layer, adapt_fmt f);
+/* Drop probability p of layer l's output (after pooling), 0 for none: the forward pass puts it through
+ * adapt_dropout in place, in the layer's own format and with the random stream rng.stream + 2^20 + 8 l + 7,
+ * and the backward pass puts the layer's output gradient (ADAPT_NT_DA) through the same draws before
+ * anything else, giving up as many fractional bits (ADAPT_NT_EXP) as the scale 1/(1 - p) needs: 1 for
+ * 0 < p <= 1/2.  For evaluation set it to 0.  p as in adapt_dropout; not the last layer's (ADAPT_EINVAL).
+ * Needs a forward pass before the next backward pass. */
+int adapt_net_set_dropout(adapt_net *net, int layer, double p);
 /* Where a tensor of the chain lives: byte offset into the workspace, element count, bytes per
  * element (for reading results; host pointers out). */
 int adapt_net_tensor(const adapt_net *net, int layer, int which, size_t *offset, size_t *count,

@@ -47,11 +47,12 @@ import numpy as np
 
 from . import conv_oracle as co
 from . import fxp_oracle as orc
+from . import head_oracle as head
 from . import net_oracle as no
 from . import sgd_oracle as so
 from . import wide_oracle as wo
 
-X_BN, X_BNB, X_GAP, X_MERGE = 0, 1, 2, 3
+X_BN, X_BNB, X_GAP, X_MERGE, X_DROP = 0, 1, 2, 3, 7
 
 
 def stream_x(stream0: int, layer: int, slot: int) -> int:
@@ -233,8 +234,9 @@ def _src(l: int, node) -> int:
     return node.src if node.src >= 0 else l - 1              # -1: the network input
 
 
-def forward(nodes, fmts, wq, bn_params, x, eps: float, seed: int, stream0: int):
-    """bn_params[l] = (gamma, beta) fp32 or None.  Returns dict(a_in, yc[], y[], a[], bn[] states)."""
+def forward(nodes, fmts, wq, bn_params, x, eps: float, seed: int, stream0: int, drop=None):
+    """bn_params[l] = (gamma, beta) fp32 or None; drop: {layer: drop probability of its output}.  Returns dict(a_in, yc[],
+    y[], a[], bn[] states)."""
     n = x.shape[0]
     wl0, fl0 = fmts[0]
     a_in = orc.quantize(np.asarray(x, np.float32), wl0, fl0, orc.SR, seed, no.stream_of(stream0, 0, no.SLOT_IN))[0].reshape(x.shape)
@@ -262,12 +264,17 @@ def forward(nodes, fmts, wq, bn_params, x, eps: float, seed: int, stream0: int):
             cur = gap_forward(y, wl, seed, stream_x(stream0, l, X_GAP)).reshape(n, 1, 1, L.k)
         else:
             cur = y
+        if drop and l in drop:
+            cur = head.dropout(cur, fl, drop[l], wl, fl, seed=seed, stream=stream_x(stream0, l, X_DROP))
+            if not L.pool and not L.gap:
+                ys[l] = cur                                   # the layer's output is stored once
         acts.append(cur)
     return {"a_in": a_in, "yc": yc, "y": ys, "a": acts, "bn": states}
 
 
-def backward(nodes, fmts, wq, fwd, dlogits, dlogits_fl: int, seed: int, stream0: int):
-    """Returns dict(g[], sumsq[], e_g[] exponents of the weight gradients, dgamma[], dbeta[], da[], e_da[], dyc[])."""
+def backward(nodes, fmts, wq, fwd, dlogits, dlogits_fl: int, seed: int, stream0: int, drop=None, drop_stream0=None):
+    """drop, drop_stream0: the forward pass's, whose draws are taken again (drop_stream0 = None: stream0): the gradient of a
+    layer's output passes the same dropout, with as many fractional bits fewer as the scale needs.  Returns dict(g[], sumsq[], e_g[] exponents of the weight gradients, dgamma[], dbeta[], da[], e_da[], dyc[])."""
     nl = len(nodes)
     n = fwd["a_in"].shape[0]
     g, sumsq, e_g = [None] * nl, [0] * nl, [0] * nl
@@ -297,6 +304,13 @@ def backward(nodes, fmts, wq, fwd, dlogits, dlogits_fl: int, seed: int, stream0:
         wl, fl = fmts[l]
         d, e = da[l], e_da[l]
         assert d is not None, f"layer {l} has no consumer"
+        if drop and l in drop:
+            up = 0
+            while (65536 - head.drop_threshold(drop[l])) << up < 65536:
+                up += 1
+            d = head.dropout(d, up, drop[l], wl, 0, seed=seed, stream=stream_x(stream0 if drop_stream0 is None else drop_stream0, l, X_DROP))
+            e -= up
+            da[l], e_da[l] = d, e
         if L.gap:
             d, up = gap_backward(d.reshape(n, L.k), L.p, L.q)
             e += up

@@ -213,6 +213,7 @@ def load_library():
     lib.adapt_net_precision_switch.argtypes = [vp, dbl, Rng, C.POINTER(SwitchReport), C.POINTER(i)]
     lib.adapt_net_destroy.argtypes = [vp]
     lib.adapt_net_set_format.argtypes = [vp, i, Fmt]
+    lib.adapt_net_set_dropout.argtypes = [vp, i, dbl]
     lib.adapt_net_tensor.argtypes = [vp, i, i, C.POINTER(sz), C.POINTER(sz), C.POINTER(i)]
     lib.adapt_net_quantize_weights.argtypes = [vp, Rng]
     lib.adapt_net_forward.argtypes = [vp, vp, Rng]
@@ -885,6 +886,10 @@ class Net:
 
     def set_format(self, layer, wl, fl):
         _check(self._lib.adapt_net_set_format(self._h, layer, Fmt(wl, fl)), "adapt_net_set_format")
+
+    def set_dropout(self, layer, p):
+        """Drop probability of the layer's output in training; 0 for evaluation."""
+        _check(self._lib.adapt_net_set_dropout(self._h, layer, p), "adapt_net_set_dropout")
 
     def tensor(self, layer, which):
         """View of one of the chain's tensors inside the workspace (flat int8 / int16; NT_STATS: a NetStats copy)."""

@@ -505,12 +505,13 @@ constexpr size_t kExpBytes = 32;       // per layer: exponents of da, of the gra
 
 // random streams of the steps that only residual / batch-norm networks have
 constexpr uint64_t kStreamX = (uint64_t)1 << 20;
-enum { X_BN = 0, X_BNB = 1, X_GAP = 2, X_MERGE = 3 };
+enum { X_BN = 0, X_BNB = 1, X_GAP = 2, X_MERGE = 3 /* to 6: at most four consumers */, X_DROP = 7 };
 
 struct NetLayer {
     adapt_layer_desc d;
     int bn, src, res, gap;    // src: the layer that feeds the convolution (-1: the network input); res: shortcut layer or -1
     adapt_fmt fmt;
+    double drop;              // drop probability of the layer's output (0: none)
     float *w;                 // master weights (caller's)
     float *gamma, *beta;      // batch-norm parameters (caller's) or null
     int p, q;                 // contraction output size
@@ -578,6 +579,7 @@ bool plan_net(const adapt_node_desc *descs, int count, int lb_upr, int wl_max, s
         if (y.res >= 0 && !y.bn) return false;                     // the shortcut is added inside the batch-norm output
         if (y.gap && y.d.pool) return false;
         y.fmt = adapt_fmt{8, 4};
+        y.drop = 0.0;
         y.w = nullptr;
         y.gamma = y.beta = nullptr;
         y.p = (c.h + 2 * c.pad - c.r) / c.stride + 1;
@@ -648,6 +650,7 @@ struct adapt_net {
     double bn_eps;
     int wl_max;               // 16, or 32 for a chain laid out for int32 codes
     bool forward_done, backward_done;
+    adapt_rng forward_rng;    // of the last forward pass: the backward pass takes the draws of its dropout again
     int dlogits_fl;
     // precision switch
     bool has_switch;
@@ -842,6 +845,14 @@ extern "C" int adapt_net_set_format(adapt_net *net, int layer, adapt_fmt f)
     return ADAPT_OK;
 }
 
+extern "C" int adapt_net_set_dropout(adapt_net *net, int layer, double p)
+{
+    if (!net || layer < 0 || layer >= (int)net->L.size() - 1 || !(p >= 0.0 && p < 1.0) || p * 65536.0 + 0.5 >= 65536.0) return ADAPT_EINVAL;
+    net->L[layer].drop = p;
+    net->forward_done = net->backward_done = false;
+    return ADAPT_OK;
+}
+
 extern "C" int adapt_net_tensor(const adapt_net *net, int layer, int which, size_t *offset, size_t *count, int *elem_bytes)
 {
     if (!net || !offset || !count || !elem_bytes) return ADAPT_EINVAL;
@@ -918,7 +929,11 @@ extern "C" int adapt_net_forward(adapt_net *net, const float *x, adapt_rng rng)
             if (int s = adapt_maxpool2_fwd(ctx, net->ws + y.off_y, y.fmt, c.n, y.p, y.q, c.k, net->ws + y.off_a)) return s;
         if (y.gap)
             if (int s = adapt_gap_fwd(ctx, net->ws + y.off_y, y.fmt, c.n, y.p * y.q, c.k, slot_rng_x(rng, l, X_GAP), net->ws + y.off_a)) return s;
+        if (y.drop > 0.0)
+            if (int s = adapt_dropout(ctx, net->ws + y.off_a, y.fmt, y.n_a, y.drop, y.fmt, slot_rng_x(rng, l, X_DROP), nullptr, y.fmt, net->ws + y.off_a))
+                return s;
     }
+    net->forward_rng = rng;
     net->forward_done = true;
     return ADAPT_OK;
 }
@@ -956,6 +971,17 @@ extern "C" int adapt_net_backward(adapt_net *net, const void *dlogits, int dlogi
         ExpRec *ex_l = net->exps(l);
         const void *da = (l == count - 1) ? dlogits : net->ws + y.off_da;
         const long long *e_cur = &ex_l->e_da;
+        if (y.drop > 0.0) {
+            // the scale 2^16 / K takes `up` fractional bits, so that nothing saturates
+            const int keep = 65536 - (int)std::floor(y.drop * 65536.0 + 0.5);
+            int up = 0;
+            while ((keep << up) < 65536) ++up;
+            adapt_rng draws = slot_rng_x(net->forward_rng, l, X_DROP);
+            draws.mode = rng.mode;
+            char *own = net->ws + y.off_da;
+            if (int s = adapt_dropout(ctx, own, adapt_fmt{y.fmt.wl, up}, y.n_a, y.drop, adapt_fmt{y.fmt.wl, 0}, draws, nullptr, y.fmt, own)) return s;
+            if (up > 0) hipLaunchKernelGGL(exp_set_kernel, dim3(1), dim3(1), 0, ctx->stream, &ex_l->e_da, (const long long *)&ex_l->e_da, (long long)-up);
+        }
         if (y.gap) {
             int up = 0;
             while ((1 << up) < y.p * y.q) ++up;
