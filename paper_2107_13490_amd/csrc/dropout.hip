@@ -8,6 +8,7 @@
 
 #include <algorithm>
 
+#include "code_vec.hpp"
 #include "common.hpp"
 #include "context.hpp"
 
@@ -39,36 +40,6 @@ __device__ __forceinline__ long long drop_one(long long x, int up, int drop, int
     const long long t = X + (mode == ADAPT_SR ? (int)r16 - drop : keep >> 1);
     const long long q = t / keep;
     return q - (q * keep > t);                             // towards minus infinity
-}
-
-// ---- eight codes at any address of their element size (the device loads and stores unaligned vectors) ----
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, int (&c)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-        __builtin_memcpy(c, p, 32);
-    } else {
-        uint32_t w[2 * sizeof(T)];
-        __builtin_memcpy(w, p, sizeof(w));
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            c[j] = sizeof(T) == 1 ? (int)(int8_t)(w[j >> 2] >> (8 * (j & 3))) : (int)(int16_t)(w[j >> 1] >> (16 * (j & 1)));
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const int (&c)[8])
-{
-    if constexpr (sizeof(T) == 4) {
-        __builtin_memcpy(p, c, 32);
-    } else {
-        uint32_t w[2 * sizeof(T)];
-#pragma unroll
-        for (int k = 0; k < (int)(2 * sizeof(T)); ++k)
-            w[k] = sizeof(T) == 1 ? (uint32_t)(c[4 * k] & 0xff) | ((uint32_t)(c[4 * k + 1] & 0xff) << 8) | ((uint32_t)(c[4 * k + 2] & 0xff) << 16) |
-                                        ((uint32_t)c[4 * k + 3] << 24)
-                                  : (uint32_t)(c[2 * k] & 0xffff) | ((uint32_t)c[2 * k + 1] << 16);
-        __builtin_memcpy(p, w, sizeof(w));
-    }
 }
 
 // What bounds it: 8-bit codes the vector units (a Philox block is 19 64-bit products and 20 three-way xors for 8 elements, 12 of
@@ -137,6 +108,16 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a,
     };
     auto group = [&](uint64_t g, const int (&c)[8], const int (&r)[8]) {
         const u32x4 blk = rounding_block(a.seed, a.stream, g);
+        if constexpr (HOW == BY_TABLE && !RES && sizeof(TO) < 4) {
+            uint32_t sum[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t r16 = lane16(blk, e);
+                sum[e] = (int)r16 >= k.drop ? table[c[e] & 255] + r16 : 0;
+            }
+            store_upper(out + 8 * g, sum);
+            return;
+        }
         int v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = one(c[e], r[e], lane16(blk, e));

@@ -2,6 +2,7 @@
 // fixed-point codes.
 #include <algorithm>
 
+#include "code_vec.hpp"
 #include "common.hpp"
 #include "context.hpp"
 
@@ -318,15 +319,21 @@ __global__ void __launch_bounds__(kMostThreads) cross_entropy_kernel(const Logit
     for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) {
         uint32_t w[W];
         load_unit(body + (uint64_t)u * U, w);
-        G q[U];
+        uint32_t q[U];      // codes; of at most 16 bits: in the upper halves
 #pragma unroll
         for (int h = 0; h < U / 8; ++h) {
             u32x4 blk = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
             if (a.mode == ADAPT_SR) blk = rounding_block(a.seed, a.stream, group0 + (uint64_t)u * (U / 8) + h);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[8 * h + e] = code_at(unit_get<T>(w, 8 * h + e), lane16(blk, e));
+            for (int e = 0; e < 8; ++e) {
+                const T l = unit_get<T>(w, 8 * h + e);
+                if constexpr (sizeof(G) == 4) q[8 * h + e] = (uint32_t)code_at(l, lane16(blk, e));
+                else q[8 * h + e] = (uint32_t)(kByte ? codes32[(uint8_t)l] : (int)grid_of(ex.at(l, m))) + lane16(blk, e);
+            }
         }
-        __builtin_memcpy(grad + head + (first + u) * U, q, sizeof(q));
+        G *to = grad + head + (first + u) * U;
+        if constexpr (sizeof(G) == 4) __builtin_memcpy(to, q, sizeof(q));
+        else store_upper(to, q);
     }
     if (on_edge) grad[edge_col] = code_at(edge, rounding_bits_of(a.seed, a.stream, base + edge_col, a.mode));
     // the label's own element, by the thread that has just stored it among others
