@@ -184,7 +184,7 @@ template <typename T>
 __device__ __forceinline__ void load_unit(const T *p, uint32_t (&w)[kWords<T>]) { __builtin_memcpy(w, p, kUnit<T> * sizeof(T)); }
 
 template <typename T, typename G, int MODE>
-__global__ void __launch_bounds__(kMostThreads) cross_entropy_kernel(const LogitArgs a, const ChunkArgs c)
+__global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const LogitArgs a, const ChunkArgs c)
 {
     constexpr int U = kUnit<T>, W = kWords<T>;
     constexpr bool kByte = sizeof(T) == 1, kFloat = __is_same(T, float);
@@ -504,7 +504,7 @@ __device__ __forceinline__ void rebase(LogPart &p, double r)
 }
 
 template <typename T, bool TOP, bool FIXED>
-__global__ void __launch_bounds__(kMostThreads) log_probs_kernel(const LogitArgs a, const LogChunkArgs c)
+__global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitArgs a, const LogChunkArgs c)
 {
     constexpr int U = kUnit<T>, W = kWords<T>;
     constexpr bool kFloat = __is_same(T, float);
