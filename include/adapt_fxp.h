@@ -557,7 +557,7 @@ int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows
  *             value (evaluated in 64 bits), with the random bits of element i*classes + j.
  *             0 in rows without label.  Must not overlap the logits
  *   weights   device float[rows], or NULL for 1 everywhere (a mean over the rows is a power of two in
- *             fg.fl and a weight)
+ *             fg.fl and a weight).  A row whose weight is not finite has a gradient of 0
  * |p - [..]| <= 1, so fg.fl = fg.wl - 1 loses nothing but the code of exactly 1.
  * Workspace: adapt_workspace_bytes with ADAPT_CALL_CROSS_ENTROPY. */
 int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes,

@@ -33,8 +33,8 @@ __device__ __forceinline__ void store8(T *p, const int (&c)[8])
     }
 }
 
-// Codes from sums z + R in units of 2^-16: the upper halves of the sums, or their lower bytes, side by side
-template <typename G, int N>
+// Codes from sums z + R in units of 2^-16: the upper halves of the sums, or their lower bytes, side by side.  PAST: past the caches
+template <bool PAST, typename G, int N>
 __device__ __forceinline__ void store_upper(G *p, const uint32_t (&t)[N])
 {
     uint32_t w[N * sizeof(G) / 4];
@@ -47,7 +47,14 @@ __device__ __forceinline__ void store_upper(G *p, const uint32_t (&t)[N])
             w[k] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
         }
     }
-    __builtin_memcpy(p, w, sizeof(w));
+    if constexpr (PAST) {
+        typedef uint32_t vec __attribute__((ext_vector_type(N * sizeof(G) / 4), aligned(1)));
+        vec v;
+        __builtin_memcpy(&v, w, sizeof(w));
+        __builtin_nontemporal_store(v, reinterpret_cast<vec *>(p));
+    } else {
+        __builtin_memcpy(p, w, sizeof(w));
+    }
 }
 
 }  // namespace adapt

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a,
                 const uint32_t r16 = lane16(blk, e);
                 sum[e] = (int)r16 >= k.drop ? table[c[e] & 255] + r16 : 0;
             }
-            store_upper(out + 8 * g, sum);
+            store_upper<false>(out + 8 * g, sum);
             return;
         }
         int v[8];

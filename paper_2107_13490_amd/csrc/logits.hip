@@ -12,6 +12,7 @@ constexpr int kMaxTop = 32;
 
 struct LogitArgs {
     const void *logits;
+    uint64_t row0;               // first row of the launch
     uint64_t rows, classes, ld;
     int fl;
     const int64_t *labels;
@@ -40,6 +41,14 @@ __device__ __forceinline__ uint32_t order_of(float v)
 }
 // larger first, then the lower index; never 0 (indices are below 2^30)
 __device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t index) { return ((uint64_t)order << 32) | (0x7fffffffu - index); }
+
+// log of a positive number, good to 2^-23 (absolutely, where the result is below 1): the fp32 logarithm of its mantissa
+__device__ __forceinline__ double log_of_sum(double s)
+{
+    int k;
+    const float m = (float)frexp(s, &k);
+    return fma((double)k, 0.69314718055994530942, (double)logf(m));
+}
 
 // ---------------------------------------------------------------------------------------------
 // Cross entropy.  A block takes a row, or one chunk of a long one: the largest logit (int16 and wider), the sum of the
@@ -178,6 +187,7 @@ struct ChunkArgs {
     RowPart *part;                    // [row][chunk]
     bool fixed;                       // the reference is the code `top`
     int top;
+    bool past;                        // codes are stored past the caches
 };
 
 template <typename T>
@@ -194,8 +204,8 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     __shared__ T part_m[kMostThreads / kWave];
     __shared__ int64_t codes64[kByte && sizeof(G) == 4 ? 256 : 1];
     __shared__ int32_t codes32[kByte && sizeof(G) < 4 ? 256 : 1];
-    const uint64_t i = blockIdx.x / c.splits;
-    const uint32_t chunk = blockIdx.x - (uint32_t)i * c.splits;
+    const uint32_t in_launch = blockIdx.x / c.splits, chunk = blockIdx.x - in_launch * c.splits;
+    const uint64_t i = a.row0 + in_launch;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
     const uint64_t base = i * a.classes;
     const uint32_t head = (uint32_t)min((uint64_t)(-base & (U - 1)), a.classes);
@@ -294,10 +304,16 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
         no_gradient(sum != sum ? NAN : -INFINITY);
         return;
     }
-    if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = (float)(value_of(row[label], a.fl) - ref - log(sum));
+    const double weight = a.weights ? (double)a.weights[i] : 1.0;
+    const float logp = (float)(value_of(row[label], a.fl) - ref - log_of_sum(sum));
+    if (!(fabs(weight) < INFINITY)) {
+        no_gradient(logp);
+        return;
+    }
+    if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = logp;
     // floor of the clamped value in units of 2^-16 of a code, and the code for a draw
     const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0;
-    const double scale = (a.weights ? (double)a.weights[i] : 1.0) * ldexp(1.0, a.fl_g + 16) / sum;
+    const double scale = weight * ldexp(1.0, a.fl_g + 16) / sum;
     const auto grid_of = [&](double t) { return floor(fmin(fmax(t * scale, tmin), tmax)); };
     const auto code_of = [](double z, uint32_t r16) -> int {
         if constexpr (sizeof(G) == 4) return (int)(((long long)z + r16) >> 16);
@@ -333,7 +349,8 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
         }
         G *to = grad + head + (first + u) * U;
         if constexpr (sizeof(G) == 4) __builtin_memcpy(to, q, sizeof(q));
-        else store_upper(to, q);
+        else if (c.past) store_upper<true>(to, q);
+        else store_upper<false>(to, q);
     }
     if (on_edge) grad[edge_col] = code_at(edge, rounding_bits_of(a.seed, a.stream, base + edge_col, a.mode));
     // the label's own element, by the thread that has just stored it among others
@@ -445,14 +462,6 @@ __device__ __forceinline__ void one_by_one(int k, TopScratch &s, const Every &ev
     }
 }
 
-// log of a positive number, good to 2^-23 (absolutely, where the result is below 1): the fp32 logarithm of its mantissa
-__device__ __forceinline__ double log_of_sum(double s)
-{
-    int k;
-    const float m = (float)frexp(s, &k);
-    return fma((double)k, 0.69314718055994530942, (double)logf(m));
-}
-
 // a row's label and its logit, loaded before they are needed
 template <typename T>
 struct LabelOf {
@@ -513,8 +522,8 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
     __shared__ TopScratch top;
     __shared__ double part_r[kMostThreads / kWave];
     __shared__ Pair part_s[kMostThreads / kWave];
-    const uint64_t i = blockIdx.x / c.splits;
-    const uint32_t chunk = blockIdx.x - (uint32_t)i * c.splits;
+    const uint32_t in_launch = blockIdx.x / c.splits, chunk = blockIdx.x - in_launch * c.splits;
+    const uint64_t i = a.row0 + in_launch;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
     // units start at 16-byte addresses
     const uint32_t head = (uint32_t)min((uint64_t)((-(uintptr_t)row & 15) / sizeof(T)), a.classes);
@@ -651,7 +660,9 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
     if (TOP && (int)threadIdx.x < a.topk) c.keys[(uint64_t)blockIdx.x * a.topk + threadIdx.x] = top.best[threadIdx.x];
 }
 
-// Rows of up to kSmall classes: a wavefront each, whose lanes hold their logits
+// Rows of up to kSmall classes: a wavefront each, whose lanes hold their logits.  us in a captured graph, this / a block per row:
+// 256 x 100 log probabilities of 8 bits 3.0 / 3.1, with 5 alternatives 4.7 / 8.2, cross entropy 4.0 / 5.0; 8192 x 100 5.1 / 6.0, 9.6 / 24,
+// 8.2 / 12.8.  At 256 classes (8192 rows) they meet: 5.9 / 5.9, 10.7 / 23, 11.5 / 11.7.
 constexpr int kSmall = 256, kSmallThreads = 256;
 
 template <typename T>
@@ -687,7 +698,7 @@ __global__ void __launch_bounds__(kSmallThreads) log_probs_small_kernel(const Lo
 {
     typedef typename RowValue<T>::type V;
     constexpr int N = SmallRow<T>::N;
-    const uint64_t i = (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
+    const uint64_t i = a.row0 + (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
     if (i >= a.rows) return;
     const int lane = threadIdx.x & (kWave - 1), classes = (int)a.classes;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
@@ -723,7 +734,7 @@ template <typename T, typename G>
 __global__ void __launch_bounds__(kSmallThreads) cross_entropy_small_kernel(const LogitArgs a)
 {
     constexpr int N = SmallRow<T>::N;
-    const uint64_t i = (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
+    const uint64_t i = a.row0 + (uint64_t)blockIdx.x * (kSmallThreads / kWave) + threadIdx.x / kWave;
     if (i >= a.rows) return;
     const int lane = threadIdx.x & (kWave - 1), classes = (int)a.classes;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
@@ -739,9 +750,9 @@ __global__ void __launch_bounds__(kSmallThreads) cross_entropy_small_kernel(cons
         s += e[k];
     }
     s = wave_sum(s);
-    const bool counts = there && x.m > -INFINITY;
+    const bool counts = there && x.m > -INFINITY && fabs(weight) < INFINITY;
     if (lane == 0 && a.logp)
-        a.logp[i] = label < 0 ? 0.0f : !there || x.m != x.m ? NAN : x.m == -INFINITY ? -INFINITY : (float)(at_label - x.m - log(s));
+        a.logp[i] = label < 0 ? 0.0f : !there || x.m != x.m ? NAN : x.m == -INFINITY ? -INFINITY : (float)(at_label - x.m - log_of_sum(s));
     const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0, scale = weight * ldexp(1.0, a.fl_g + 16) / s;
     G *grad = static_cast<G *>(a.grad) + i * a.ldg;
 #pragma unroll
@@ -875,6 +886,17 @@ using namespace adapt;
 
 static int logit_bytes(adapt_fmt f) { return f.wl == ADAPT_WL_FP32 ? 4 : storage_bytes(f); }
 
+// A launch takes fewer than 2^32 threads: rows in slabs of 2^21 blocks (rows in chunks are fewer)
+template <typename Launch>
+static void for_slabs(LogitArgs a, uint64_t rows_per_block, const Launch &launch)
+{
+    const uint64_t most = rows_per_block << 21;
+    for (a.row0 = 0; a.row0 < a.rows; a.row0 += most) {
+        const uint64_t rows = std::min(a.rows - a.row0, most);
+        launch(a, (unsigned)((rows + rows_per_block - 1) / rows_per_block));
+    }
+}
+
 template <typename T>
 static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsPlan &p, int wl)
 {
@@ -882,14 +904,17 @@ static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsP
     const bool fixed = !__is_same(T, float) && span - 1 - a.fl <= 4;
     LogChunkArgs c = {p.splits, p.units, reinterpret_cast<LogPart *>(scratch(ctx)), reinterpret_cast<uint64_t *>(scratch(ctx) + p.part_bytes),
                       (int)(4 * p.threads)};
-    const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
+    const dim3 block(p.threads);
     const size_t lds = a.topk > 0 ? c.listed * sizeof(uint64_t) : 0;
-    if constexpr (!__is_same(T, float)) {
-        if (fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, true>), grid, block, lds, ctx->stream, a, c);
-        else if (fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, true>), grid, block, lds, ctx->stream, a, c);
-    }
-    if (!fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, false>), grid, block, lds, ctx->stream, a, c);
-    else if (!fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, false>), grid, block, lds, ctx->stream, a, c);
+    for_slabs(a, 1, [&](const LogitArgs &s, unsigned rows) {
+        const dim3 grid(rows * p.splits);
+        if constexpr (!__is_same(T, float)) {
+            if (fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, true>), grid, block, lds, ctx->stream, s, c);
+            else if (fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, true>), grid, block, lds, ctx->stream, s, c);
+        }
+        if (!fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, false>), grid, block, lds, ctx->stream, s, c);
+        else if (!fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, false>), grid, block, lds, ctx->stream, s, c);
+    });
     if (p.splits > 1) {
         c.listed = 1024;
         hipLaunchKernelGGL(join_log_probs_kernel<T>, dim3((unsigned)a.rows), dim3(kJoinThreads), a.topk ? c.listed * sizeof(uint64_t) : 0, ctx->stream, a, c);
@@ -913,16 +938,18 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     a.labels = labels; a.logp = logp; a.lse = lse; a.entropy = entropy;
     a.topk = topk; a.top_index = top_index; a.top_logp = top_logp;
     if (classes <= (size_t)kSmall) {
-        const dim3 grid((unsigned)((rows + kSmallThreads / kWave - 1) / (kSmallThreads / kWave))), block(kSmallThreads);
-        if (f.wl == ADAPT_WL_FP32) hipLaunchKernelGGL(log_probs_small_kernel<float>, grid, block, 0, ctx->stream, a);
-        else if (f.wl <= 8) hipLaunchKernelGGL(log_probs_small_kernel<int8_t>, grid, block, 0, ctx->stream, a);
-        else if (f.wl <= 16) hipLaunchKernelGGL(log_probs_small_kernel<int16_t>, grid, block, 0, ctx->stream, a);
-        else hipLaunchKernelGGL(log_probs_small_kernel<int32_t>, grid, block, 0, ctx->stream, a);
+        const dim3 block(kSmallThreads);
+        for_slabs(a, kSmallThreads / kWave, [&](const LogitArgs &s, unsigned blocks) {
+            const dim3 grid(blocks);
+            if (f.wl == ADAPT_WL_FP32) hipLaunchKernelGGL(log_probs_small_kernel<float>, grid, block, 0, ctx->stream, s);
+            else if (f.wl <= 8) hipLaunchKernelGGL(log_probs_small_kernel<int8_t>, grid, block, 0, ctx->stream, s);
+            else if (f.wl <= 16) hipLaunchKernelGGL(log_probs_small_kernel<int16_t>, grid, block, 0, ctx->stream, s);
+            else hipLaunchKernelGGL(log_probs_small_kernel<int32_t>, grid, block, 0, ctx->stream, s);
+        });
         return hip_status(ctx, hipGetLastError());
     }
     const LogProbsPlan p = plan_log_probs(ctx->num_cu, rows, classes, topk, f);
     if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
-    if (rows * p.splits >= (1ull << 31)) return ADAPT_EUNSUPPORTED;
     if (f.wl == ADAPT_WL_FP32) launch_log_probs<float>(ctx, a, p, f.wl);
     else if (f.wl <= 8) launch_log_probs<int8_t>(ctx, a, p, f.wl);
     else if (f.wl <= 16) launch_log_probs<int16_t>(ctx, a, p, f.wl);
@@ -933,21 +960,29 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
 template <typename T, typename G>
 static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
 {
+    // Codes of 96 MiB or more leave the caches before the next call reads them, and take the room that the sweeps need.  us, in the
+    // caches / past them, alone and with a copy of the codes behind: 62 MiB (2048 x 32000, 8 bits) 33.5 / 33.4, 51 / 57; 125 MiB (4096)
+    // 74 / 60, 127 / 123; 128 MiB (1024 x 65531, 16 bits) 83 / 66, 133 / 126; 250 MiB (8192 x 32000, 8 bits) 134 / 127, 231 / 229
+    const bool past = a.rows * a.classes * sizeof(G) >= ((uint64_t)96 << 20);
     // distances to the largest code: of the storage for int16 (they index tables), of the format for int32
     const int span = sizeof(T) == 2 ? 16 : wl;
     if (a.classes <= (uint64_t)kSmall) {
-        constexpr int kRows = kSmallThreads / kWave;
-        hipLaunchKernelGGL((cross_entropy_small_kernel<T, G>), dim3((unsigned)((a.rows + kRows - 1) / kRows)), dim3(kSmallThreads), 0, ctx->stream, a);
+        for_slabs(a, kSmallThreads / kWave, [&](const LogitArgs &s, unsigned blocks) {
+            hipLaunchKernelGGL((cross_entropy_small_kernel<T, G>), dim3(blocks), dim3(kSmallThreads), 0, ctx->stream, s);
+        });
         return;
     }
-    const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), span - a.fl <= 9, (int)((1ll << (span - 1)) - 1)};
-    const dim3 grid((unsigned)(a.rows * p.splits)), block(p.threads);
-    if (p.splits == 1) {
-        hipLaunchKernelGGL((cross_entropy_kernel<T, G, WHOLE_ROW>), grid, block, 0, ctx->stream, a, c);
-    } else {
-        hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_SUMS>), grid, block, 0, ctx->stream, a, c);
-        hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_CODES>), grid, block, 0, ctx->stream, a, c);
-    }
+    const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), span - a.fl <= 9, (int)((1ll << (span - 1)) - 1), past};
+    const dim3 block(p.threads);
+    for_slabs(a, 1, [&](const LogitArgs &s, unsigned rows) {
+        const dim3 grid(rows * p.splits);
+        if (p.splits == 1) {
+            hipLaunchKernelGGL((cross_entropy_kernel<T, G, WHOLE_ROW>), grid, block, 0, ctx->stream, s, c);
+        } else {
+            hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_SUMS>), grid, block, 0, ctx->stream, s, c);
+            hipLaunchKernelGGL((cross_entropy_kernel<T, G, CHUNK_CODES>), grid, block, 0, ctx->stream, s, c);
+        }
+    });
 }
 template <typename T>
 static void launch_cross_entropy_to(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
@@ -977,7 +1012,6 @@ extern "C" int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt
     a.wl_g = fg.wl; a.fl_g = fg.fl; a.mode = rng.mode; a.seed = rng.seed; a.stream = rng.stream;
     const CrossEntropyPlan p = plan_cross_entropy(ctx->num_cu, rows, classes, f);
     if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
-    if (rows * p.splits >= (1ull << 31)) return ADAPT_EUNSUPPORTED;
     if (f.wl == ADAPT_WL_FP32) launch_cross_entropy_to<float>(ctx, a, p, 0);
     else if (f.wl <= 8) launch_cross_entropy_to<int8_t>(ctx, a, p, f.wl);
     else if (f.wl <= 16) launch_cross_entropy_to<int16_t>(ctx, a, p, f.wl);

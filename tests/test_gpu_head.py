@@ -228,6 +228,38 @@ def test_many_rows():
         _check_cross_entropy(x, f, y, (8, 7))
 
 
+def test_weights_of_every_kind():
+    rng = np.random.default_rng(8)
+    w = np.array([0.0, -0.0, -1.5, 3e38, -3e38, np.inf, -np.inf, np.nan, 1e-40, 2.0], dtype=np.float32)
+    finite = np.where(np.isfinite(w), w, 0).astype(np.float32)
+    for rows, classes, wl in ((10, 90, 8), (10, 3001, 8), (10, 3001, 16), (10, 3001, 0), (10, 70001, 0)):
+        x, y = _logits(rng, rows, classes, wl, _fl(wl)), rng.integers(0, classes, rows)
+        f = (wl, _fl(wl)) if wl else None
+        got, logp = ctx().cross_entropy(dev(x), f, dev(y), (12, 11), weights=dev(w), seed=3, stream=5)
+        want = head.quantize_real(head.gradient(x, f[1] if f else None, y, finite), 12, 11, seed=3, stream=5)
+        assert np.array_equal(host(got), want)
+        assert np.isfinite(host(logp)).all()
+
+
+@pytest.mark.parametrize("rows,classes", [((1 << 21) + 5, 300), ((1 << 23) + 9, 3)])
+def test_more_rows_than_a_launch_takes(rows, classes):
+    """Rows around the seam and at the end, against calls on those rows alone (nearest rounding: no draws)."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randint(-60, 60, (rows, classes), generator=g, device="cuda", dtype=torch.int8)
+    y = torch.randint(-1, classes, (rows,), generator=g, device="cuda")
+    c = ctx()
+    lp = c.log_probs(x, (8, 4), y, topk=2)
+    dl, logp = c.cross_entropy(x, (8, 4), y, (8, 7), mode=pkg.RN_HALF_UP)
+    seam = 1 << (21 if classes > 256 else 23)
+    for a, b in ((0, 4), (seam - 3, seam + 3), (rows - 4, rows)):
+        want = c.log_probs(x[a:b], (8, 4), y[a:b], topk=2)
+        for k in want:
+            assert torch.equal(lp[k][a:b], want[k]), (k, a)
+        w, wp = c.cross_entropy(x[a:b].clone(), (8, 4), y[a:b], (8, 7), mode=pkg.RN_HALF_UP)
+        assert torch.equal(dl[a:b], w) and torch.allclose(logp[a:b], wp, rtol=1e-6, atol=1e-6)
+        assert torch.equal(logp[a:b] == 0, y[a:b] < 0)
+
+
 def test_gradient_against_differences_of_the_loss():
     """(L(x + h) - L(x - h)) / 2h of the oracle's loss against the codes' values: half a code step for the rounding, h^2 / 6
     for the third derivative (below 1), and the difference's own rounding, 2^-63 |L| / h."""
