@@ -735,16 +735,18 @@ class Context:
         if not t.is_contiguous():
             raise ValueError(f"{what} has strides {t.stride()}: the call takes dense tensors")
 
+    def _dense(self, t, dtype):
+        """Whether a tensor is what `_own` takes (what nearly every call passes)."""
+        return t.dtype is dtype and t.get_device() == self._device and t.is_contiguous()
+
     def _matrix(self, what, t, dtype):
         """The same for a matrix whose rows may lie further apart than they are long; returns (rows, columns, row stride)."""
         if t.dim() != 2:
             raise ValueError(f"{what} has the shape {tuple(t.shape)}: rows x classes are wanted")
-        if t.is_contiguous():
-            self._own(what, t, dtype)
-            rows, cols = t.shape
+        rows, cols = t.shape
+        if self._dense(t, dtype):
             return rows, cols, cols
         self._own(what, t[:0], dtype)
-        rows, cols = t.shape
         apart = t.stride(0) if rows > 1 else cols
         if apart < cols or (cols > 1 and t.stride(1) != 1):
             raise ValueError(f"{what} has strides {t.stride()}: the call takes rows that are dense and do not overlap")
@@ -757,14 +759,15 @@ class Context:
         fx = _fmt(fx)
         fo = fx if fo is None else _fmt(fo)
         codes = self._codes
-        self._own("x", x, codes(fx.wl))
+        if not self._dense(x, codes(fx.wl)):
+            self._own("x", x, codes(fx.wl))
         if res is None:
             fres = fx
         else:
             fres = _fmt(fres)
             self._own("res", res, codes(fres.wl), x.shape)
         if out is None:
-            out = self._torch.empty(x.shape, dtype=codes(fo.wl), device=x.device)
+            out = self._torch.empty_like(x, dtype=codes(fo.wl))
         else:
             self._own("out", out, codes(fo.wl), x.shape)
         _check(self._lib.adapt_dropout(self._h, x.data_ptr(), fx, x.numel(), p, fo, Rng(mode, seed, stream), _ptr(res), fres,
@@ -788,16 +791,22 @@ class Context:
         labels), lse, entropy (None unless asked for), top_idx int32[rows, topk], top_logp (None if topk = 0))."""
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
+        lse = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        logp = ent = idx = top = label_at = logp_at = ent_at = idx_at = top_at = None
         if labels is not None:
-            self._own("labels", labels, torch.int64, (rows,))
-        dev = logits.device
-        lse = torch.empty(rows, dtype=torch.float32, device=dev)
-        logp = torch.empty(rows, dtype=torch.float32, device=dev) if labels is not None else None
-        ent = torch.empty(rows, dtype=torch.float32, device=dev) if entropy else None
-        idx = torch.empty((rows, topk), dtype=torch.int32, device=dev) if topk > 0 else None
-        top = torch.empty((rows, topk), dtype=torch.float32, device=dev) if topk > 0 else None
-        _check(self._lib.adapt_log_probs(self._h, _ptr(logits), f, rows, classes, ld, _ptr(labels), _ptr(logp), _ptr(lse), _ptr(ent),
-                                         topk, _ptr(idx), _ptr(top)), "adapt_log_probs")
+            if not self._dense(labels, torch.int64) or labels.shape != lse.shape:
+                self._own("labels", labels, torch.int64, (rows,))
+            logp = torch.empty_like(lse)
+            label_at, logp_at = labels.data_ptr(), logp.data_ptr()
+        if entropy:
+            ent = torch.empty_like(lse)
+            ent_at = ent.data_ptr()
+        if topk > 0:
+            top = torch.empty((rows, topk), dtype=torch.float32, device=logits.device)
+            idx = torch.empty_like(top, dtype=torch.int32)
+            idx_at, top_at = idx.data_ptr(), top.data_ptr()
+        _check(self._lib.adapt_log_probs(self._h, logits.data_ptr(), f, rows, classes, ld, label_at, logp_at, lse.data_ptr(), ent_at,
+                                         topk, idx_at, top_at), "adapt_log_probs")
         return {"logp": logp, "lse": lse, "entropy": ent, "top_idx": idx, "top_logp": top}
 
     def cross_entropy(self, logits, f, labels, fg, weights=None, mode=SR, seed=0, stream=0, out=None):
@@ -807,19 +816,20 @@ class Context:
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
         fg = _fmt(fg)
-        self._own("labels", labels, torch.int64, (rows,))
+        logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        if not self._dense(labels, torch.int64) or labels.shape != logp.shape:
+            self._own("labels", labels, torch.int64, (rows,))
         if weights is not None:
             self._own("weights", weights, torch.float32, (rows,))
-        ldg = classes
+        ldg, codes = classes, self._codes(fg.wl)
         if out is None:
-            out = torch.empty((rows, classes), dtype=self._codes(fg.wl), device=logits.device)
+            out = torch.empty_like(logits, dtype=codes, memory_format=torch.contiguous_format)
         else:
             if out.shape != logits.shape:
                 raise ValueError(f"out has the shape {tuple(out.shape)}, not {tuple(logits.shape)}")
-            ldg = self._matrix("out", out, self._codes(fg.wl))[2]
-        logp = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        _check(self._lib.adapt_cross_entropy(self._h, _ptr(logits), f, rows, classes, ld, _ptr(labels), _ptr(weights), fg,
-                                             Rng(mode, seed, stream), _ptr(out), ldg, _ptr(logp)), "adapt_cross_entropy")
+            ldg = self._matrix("out", out, codes)[2]
+        _check(self._lib.adapt_cross_entropy(self._h, logits.data_ptr(), f, rows, classes, ld, labels.data_ptr(), _ptr(weights), fg,
+                                             Rng(mode, seed, stream), out.data_ptr(), ldg, logp.data_ptr()), "adapt_cross_entropy")
         return out, logp
 
 

@@ -57,6 +57,7 @@ enum { BY_TABLE, BY_I32, BY_F64 };
 
 struct DropConst {
     double d_up, d_inv, d_add;       // 2^up, 1/K, 1/2 and what makes R (nearest: 0) the u of the rule
+    int down;                        // BY_F64: bits that x loses first (its fractional bits beyond 16 more than the output's)
     float f_inv;
     int drop, keep, up;
 };
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a,
             const int rest = n - __mul24(q, k.keep);
             q += (rest >= k.keep) - (rest < 0);
         } else {
-            double y = floor(fma((double)c, k.d_up, (nearest ? 0.0 : (double)r16) + k.d_add) * k.d_inv);
+            double y = floor(fma((double)(c >> k.down), k.d_up, (nearest ? 0.0 : (double)r16) + k.d_add) * k.d_inv);
             y = stays ? y : 0.0;
             if (has_res) y += (double)res * res_scale;                   // beyond 2^53 it saturates, rounded or not
             return (int)fmin(fmax(y, lo), hi);
@@ -188,13 +189,13 @@ extern "C" int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t
     const int up = 16 + fo.fl - fx.fl, keep = 65536 - drop;
     const DropArgs a = {x, res, out, n, up, res ? fo.fl - fres.fl : 0, drop, keep, es_x, es_r, es_o, fo.wl, rng.mode, rng.seed, rng.stream};
     const bool nearest = rng.mode != ADAPT_SR;
-    const DropConst k = {std::ldexp(1.0, up), 1.0 / keep, 0.5 + (nearest ? keep >> 1 : -drop), 1.0f / (float)keep, drop, keep, up};
+    const DropConst k = {std::ldexp(1.0, std::max(up, 0)), 1.0 / keep, 0.5 + (nearest ? keep >> 1 : -drop), std::max(-up, 0), 1.0f / (float)keep, drop, keep, up};
     const uint64_t groups = (n + 7) >> 3;
     const dim3 grid((unsigned)std::min<uint64_t>((groups + kDropThreads - 1) / kDropThreads, (uint64_t)ctx->num_cu * 8)), block(kDropThreads);
     const bool in_32 = !nearest && (!res || fres.wl - 1 + a.res_up <= 29);      // the residual and its sum with a quotient
     const bool table = in_32 && fx.wl <= 8 && up >= 0 && std::ldexp(1.0, fx.wl - 1 + up) < 32767.0 * keep;
     const bool i32 = in_32 && fx.wl <= 16 && up >= 0 && fx.wl - 1 + up <= 30 && keep >= 2048;
-    if (up < 0 || fx.wl - 1 + up > 50) hipLaunchKernelGGL(dropout_i64_kernel, grid, block, 0, ctx->stream, a);
+    if (fx.wl - 1 + up > 50) hipLaunchKernelGGL(dropout_i64_kernel, grid, block, 0, ctx->stream, a);
     else if (fx.wl > 16) launch<int32_t, BY_F64, true>(ctx, grid, a, k);
     else if (fx.wl > 8) {
         if (!i32) launch<int16_t, BY_F64, true>(ctx, grid, a, k);

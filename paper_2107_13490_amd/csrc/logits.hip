@@ -97,6 +97,7 @@ struct Exponentials {
     const double *table;
     int fl;
     double step;      // 2^-fl
+    double ref;       // int32: the reference's value
 
     __device__ __forceinline__ static void build(double *table, int fl)
     {
@@ -114,7 +115,7 @@ struct Exponentials {
             const uint32_t d = (uint32_t)((int)m - (int)l);
             return table[d >> 8] * table[256 + (d & 255)];
         } else if constexpr (__is_same(T, float)) return exp_by_roots((double)l - (double)m, table);
-        else return exp_by_roots((double)((long long)l - m) * step, table);
+        else return exp_by_roots(fma((double)l, step, -ref), table);
     }
 };
 
@@ -231,7 +232,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     }
 
     X::build(table, a.fl);
-    const X ex = {table, a.fl, ldexp(1.0, -a.fl)};
+    X ex = {table, a.fl, ldexp(1.0, -a.fl), 0.0};
     T m = (T)c.top;
     if (!kByte && !kFloat && !c.fixed && MODE != CHUNK_CODES) {
         m = edge;
@@ -246,6 +247,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
         __syncthreads();
     }
 
+    ex.ref = (double)m * ex.step;
     double ref, sum;
     const auto add = [](double x, double y) { return x + y; };
     if constexpr (MODE != CHUNK_CODES) {
@@ -298,6 +300,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
         for (uint32_t j = threadIdx.x; j < c.splits; j += blockDim.x) s += p[j].m > -INFINITY ? p[j].s * exp(p[j].m - ref) : p[j].s;
         sum = over_block(s, part_s, add);
         if constexpr (!kByte) m = kFloat ? (T)ref : (T)ldexp(ref, a.fl);
+        ex.ref = ref;
     }
 
     if (sum != sum || ref == -INFINITY) {
@@ -795,16 +798,17 @@ __global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const Logi
     p.e = sums.b;
     if (__syncthreads_or(bad)) p.r = NAN;
     if (a.topk > 0) {
-        // a thread's keys are those of whole chunks, each chunk's in order
+        // a chunk's keys are in order: it is taken in `slices` of every so many, so that there are 64 largest ones to compare
         const uint64_t *keys = c.keys + i * c.splits * a.topk;
+        const uint32_t slices = min((uint32_t)a.topk, (kWave + c.splits - 1) / c.splits), heads = c.splits * slices;
+        const auto head_of = [&](uint32_t j) { return keys + (uint64_t)(j / slices) * a.topk + j % slices; };
         uint64_t mine = 0;
-        for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) mine = max(mine, keys[(uint64_t)j * a.topk]);
+        for (uint32_t j = threadIdx.x; j < heads; j += kJoinThreads) mine = max(mine, *head_of(j));
         const uint64_t bound = bound_of(mine, a.topk, top, list);
-        for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads)
-            for (int n = 0; n < a.topk; ++n) {
-                const uint64_t key = keys[(uint64_t)j * a.topk + n];
-                if (key < bound || key == 0) break;
-                put(key, top, list, c.listed);
+        if (mine >= bound)
+            for (uint32_t j = threadIdx.x; j < heads; j += kJoinThreads) {
+                const uint64_t *key = head_of(j);
+                for (uint32_t n = j % slices; n < (uint32_t)a.topk && *key >= bound && *key != 0; n += slices, key += slices) put(*key, top, list, c.listed);
             }
         __syncthreads();
         if (top.count <= (uint32_t)c.listed) {
@@ -821,18 +825,23 @@ struct LogProbsPlan {
     size_t part_bytes, ws_bytes;
 };
 
+// Threads: a thread takes two units where blocks are few (eight where they fill the card), rows of 4096 units 1024 threads where each has a
+// compute unit of its own.  Chunks: a second launch and its join pay only for few, long rows.  us in a captured graph, chunks / a
+// block per row: 1 x 100000 of 8 bits (6250 units) 6.9 / 8.0, 16 bits with 8 alternatives (12500) 12.4 / 12.3, fp32 with 32 17.1 / 17.5;
+// 1 x 200000 6.9 / 12.7, 12.5 / 18.2, 17.1 / 24.6; 64 x 100000 8.7 / 8.6, 15.3 / 13.0, 23.1 / 18.0; 64 x 200000 9.5 / 13.2, 17.2 / 19.1,
+// 25.9 / 28.6; 200 x 200000 17.3 / 15.5, 29.3 / 21.6, 49.5 / 33.9.
 static LogProbsPlan plan_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, adapt_fmt f)
 {
     const int U = f.wl != ADAPT_WL_FP32 && f.wl <= 8 ? 16 : 8;
     LogProbsPlan p = {};
-    const uint64_t all = std::max<uint64_t>(classes / U, 1);
+    const uint64_t all = std::max<uint64_t>(classes / U, 1), wanted = 4 * (uint64_t)num_cu /* blocks */;
     uint64_t splits = 1;
-    const uint64_t wanted = 4 * (uint64_t)num_cu;             // blocks
-    if (rows < wanted / 2 && all >= 512) splits = std::min<uint64_t>((wanted + rows - 1) / std::max<uint64_t>(rows, 1), all / 256);
+    if (rows > 0 && rows * 4 <= (uint64_t)num_cu && all >= 12288) splits = std::min<uint64_t>((wanted + rows - 1) / rows, all / 256);
     p.units = (uint32_t)((all + splits - 1) / splits);
     p.splits = (uint32_t)((all + p.units - 1) / p.units);
-    const uint64_t per = rows * splits >= wanted ? 8 : 2, threads = (p.units + per - 1) / per;
-    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, 512);
+    const uint64_t per = rows * splits >= wanted && splits == 1 ? 8 : 2, threads = (p.units + per - 1) / per;
+    const uint64_t most = splits == 1 && rows <= (uint64_t)num_cu && all >= 4096 ? 1024 : 512;
+    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, most);
     if (p.splits > 1) {
         p.part_bytes = (rows * p.splits * sizeof(LogPart) + 255) & ~(size_t)255;
         p.ws_bytes = p.part_bytes + rows * p.splits * topk * sizeof(uint64_t);
@@ -845,7 +854,12 @@ size_t ws_need_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, 
     return plan_log_probs(num_cu, rows, classes, topk, f).ws_bytes + 16;
 }
 
-// How the rows of a cross entropy are cut: rows too few to fill the card into chunks, whose sums are a launch of their own.
+// How the rows of a cross entropy are cut.  Chunks of a row, whose sums are a launch of their own, for few and long rows: us in a captured
+// graph, chunks / a block per row: 1 x 28723 of 8 bits (1795 units) 8.7 / 7.4, 16 bits (3590) 9.1 / 10.7, fp32 10.8 / 16.3; 64 x 28723
+// 10.1 / 8.0, 11.4 / 11.9, 13.6 / 17.4; 100 x 100000 14.6 / 15.6, 22 / 33, 31 / 54; 200 x 100000 19.9 / 16.9, 32.3 / 30.9, 47.1 / 46.9.
+// Threads: one unit each where every row has a compute unit of its own (1 x 5000, 1, 2, 4 units: 4.4, 5.0, 5.5), two where blocks are few
+// (400 x 5000 of 16 bits, 1, 2, 4: 8.2, 7.5, 8.4), otherwise eight and at most 512 threads: 256, 512, 1024 threads take 8192 x 32000 of
+// 8 bits 140, 151, 190; 1536 x 65531 of 16 bits 186, 157, 163; 1024 x 50001 fp32 129, 125, 126.
 struct CrossEntropyPlan {
     uint32_t splits, units, threads;
     size_t ws_bytes;
@@ -855,16 +869,14 @@ static CrossEntropyPlan plan_cross_entropy(int num_cu, uint64_t rows, uint64_t c
 {
     const int U = f.wl != ADAPT_WL_FP32 && f.wl <= 8 ? 16 : 8;
     CrossEntropyPlan p = {};
-    const uint64_t all = std::max<uint64_t>(classes / U, 1);
+    const uint64_t all = std::max<uint64_t>(classes / U, 1), wanted = 4 * (uint64_t)num_cu /* blocks */;
     uint64_t splits = 1;
-    const uint64_t wanted = 4 * (uint64_t)num_cu;             // blocks
-    if (rows < wanted / 2 && all >= 512) splits = std::min<uint64_t>((wanted + rows - 1) / std::max<uint64_t>(rows, 1), all / 256);
+    if (rows > 0 && rows * 2 <= (uint64_t)num_cu && all >= 3072) splits = std::min<uint64_t>((wanted + rows - 1) / rows, all / 256);
     p.splits = (uint32_t)splits;
     p.units = (uint32_t)((all + splits - 1) / splits);
-    // units per thread, us (rows x classes, bits; 256, 512, 1024 threads): 8192 x 32000, 8: 140, 151, 190; 1536 x 65531, 16: 186, 157,
-    // 163; 2048 x 32000, 24: 169, 157, 174; 1024 x 50001, fp32: 129, 125, 126; with few rows more threads: 512 x 32000, 8: 15.6, 13.8, 14.6
-    const uint64_t per = rows * splits >= wanted ? 8 : 4, threads = (p.units + per - 1) / per;
-    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, 512);
+    const bool alone = rows <= (uint64_t)num_cu;
+    const uint64_t per = splits > 1 ? 4 : alone ? 1 : rows < wanted ? 2 : 8, threads = (p.units + per - 1) / per;
+    p.threads = (uint32_t)std::min<uint64_t>((threads + kWave - 1) / kWave * kWave, splits == 1 && alone ? 1024 : 512);
     p.ws_bytes = p.splits > 1 ? rows * p.splits * sizeof(RowPart) : 0;
     return p;
 }

@@ -376,3 +376,17 @@ def test_refusals():
             call()
     with pytest.raises(pkg.AdaptError):
         c.log_probs(torch.zeros((4, 0), dtype=torch.int8, device="cuda"), (8, 4), y)
+
+
+@pytest.mark.parametrize("wl", [0, 8, 16])
+def test_fewer_chunks_than_alternatives(wl):
+    """Rows of which each is cut into fewer chunks than there are alternatives, the largest of them all in one chunk."""
+    rng = np.random.default_rng(wl)
+    rows, classes = 60, 100003 if wl != 8 else 200003
+    x = _logits(rng, rows, classes, wl, _fl(wl))
+    top = 100 if wl == 8 else 3000
+    x[0, :64], x[1, -64:] = top, top
+    x[2, classes // 2:classes // 2 + 33] = np.arange(33)[::-1] + 60
+    y = _labels(rng, rows, classes)
+    _check_log_probs(x, (wl, _fl(wl)) if wl else None, y, 32)
+    _check_cross_entropy(x[:3], (wl, _fl(wl)) if wl else None, y[:3], (8, 7))
