@@ -51,11 +51,15 @@ __device__ __forceinline__ double log_of_sum(double s)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Cross entropy.  A block takes a row, or one chunk of a long one: the largest logit (int16 and wider), the sum of the
-// exponentials, the codes.  Only the first sweep reads memory, the others find the row in the caches.  Elements come in units
-// that start where the generator's blocks of eight start, so that a unit takes whole blocks whatever the number of classes; in
-// a dense tensor units are aligned vectors, too.  What a row has before its first and behind its last whole unit are its edges,
-// one element per thread.
+// Cross entropy.  A block takes a row, or one chunk of a long one: the sum of the exponentials (with the largest logit before it
+// where the format's whole range does not do as a reference), then the codes, both in 64 bits, since a code is a floor.  Elements
+// come in units that start where the generator's blocks of eight start, so that a unit takes whole blocks whatever the number of
+// classes; in a dense tensor units are aligned vectors, too.  What a row has before its first and behind its last whole unit are
+// its edges, one element per thread.
+// What bounds it: the two sweeps and the codes in memory, and at 8 bits as much the issue of 13 instructions per element, 5 of them the
+// generator's.  The rows in flight exceed an XCD's L2, so the second sweep comes from memory as well; rows kept in LDS or registers
+// leave too few wavefronts (8192 x 32000 of 8 bits 126 -> 131 us, 2047 x 65531 of 16 bits 143 -> 162).  us (TB/s of both sweeps and the
+// codes): 8192 x 32000, 8 -> 8 bits 123 (6.4), 1535 x 65531, 16 -> 16 bits 118 (5.7), 1024 x 50001, fp32 -> 8 bits 87 (5.2); a copy runs at 5.0.
 // ---------------------------------------------------------------------------------------------
 template <typename T> constexpr int kUnit = sizeof(T) == 1 ? 16 : 8;      // elements
 template <typename T> constexpr int kWords = kUnit<T> * (int)sizeof(T) / 4;
@@ -220,14 +224,16 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     G *grad = static_cast<G *>(a.grad) + i * a.ldg;
     const int64_t label = a.labels[i];
     const bool there = label >= 0 && (uint64_t)label < a.classes;
-    const auto no_gradient = [&](float logp) {
+    const bool tells = threadIdx.x == 0 && chunk == 0 && a.logp;
+    const auto no_gradient = [&] {
         G zero[U] = {};
         for (uint32_t u = threadIdx.x; u < units; u += blockDim.x) __builtin_memcpy(grad + head + (first + u) * U, zero, sizeof(zero));
         if (on_edge) grad[edge_col] = 0;
-        if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = logp;
     };
     if (!there) {                                             // such a row is not read
-        if (MODE != CHUNK_SUMS) no_gradient(label < 0 ? 0.0f : NAN);
+        if (MODE == CHUNK_SUMS) return;
+        no_gradient();
+        if (tells) a.logp[i] = label < 0 ? 0.0f : NAN;
         return;
     }
 
@@ -303,17 +309,13 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
         ex.ref = ref;
     }
 
-    if (sum != sum || ref == -INFINITY) {
-        no_gradient(sum != sum ? NAN : -INFINITY);
-        return;
-    }
+    const bool bad = sum != sum, none = ref == -INFINITY;
+    if (tells) a.logp[i] = bad ? NAN : none ? -INFINITY : (float)(value_of(row[label], a.fl) - ref - log_of_sum(sum));
     const double weight = a.weights ? (double)a.weights[i] : 1.0;
-    const float logp = (float)(value_of(row[label], a.fl) - ref - log_of_sum(sum));
-    if (!(fabs(weight) < INFINITY)) {
-        no_gradient(logp);
+    if (bad || none || !(fabs(weight) < INFINITY)) {
+        no_gradient();
         return;
     }
-    if (threadIdx.x == 0 && chunk == 0 && a.logp) a.logp[i] = logp;
     // floor of the clamped value in units of 2^-16 of a code, and the code for a draw
     const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0;
     const double scale = weight * ldexp(1.0, a.fl_g + 16) / sum;
@@ -362,15 +364,16 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     if (mine) grad[label] = (G)code_of(grid_of(ex.at(row[label], m) - sum), rounding_bits_of(a.seed, a.stream, base + (uint64_t)label, a.mode));
 }
 
-
 // ---------------------------------------------------------------------------------------------
 // Log probabilities.  One sweep over the row (or a chunk of it): sums of e^(x - r) and (x - r) e^(x - r) in fp32 over a unit and in
-// fp64 from there on, and each thread's largest unit.  Where all of the format's values lie within +-16, r = 0; otherwise every
-// thread has a reference of its own that follows the logits where they get 8 ahead of it.
+// fp64 from there on, and each thread's largest unit.  For 8-bit codes within +-16 r = 0 (8192 x 32000: 63 instead of 78 us); otherwise
+// every thread has a reference of its own that follows the logits where they get 8 ahead of it.
 // The k largest: the threads fall into 64 groups (their lanes), and the k-th largest of the groups' maxima is a bound below
-// which none of them lies.  Few threads have anything above it; those look through their units again and put what they find
+// which none of them lies.  Few threads have anything above it; their units are spread over all threads, which put what they find
 // into a list, whose members count how many are ahead of them.  Should the list overflow (the largest logits in few places,
 // many of them), the row is swept once for each of the k.
+// What bounds it: memory from 16 bits on (4096 x 32000 53 us, 4.9 TB/s; 1000 x 50001 fp32 with 5 alternatives 39 us, 5.1), the exponentials'
+// and additions' issue at 8 bits (8192 x 32000 63 us, 4.2), with 8 alternatives 83.
 // ---------------------------------------------------------------------------------------------
 struct LogPart { double r, s, e; };      // reference (fp64 values; NaN: not a distribution), sums of a chunk
 
@@ -494,7 +497,7 @@ __device__ __forceinline__ void finish_row(const LogitArgs &a, uint64_t i, const
     const auto log_prob = [&](double x) { return bad ? NAN : none ? -INFINITY : (float)(x - p.r - log_s); };
     if (thread == 0) {
         if (a.lse) a.lse[i] = bad ? NAN : none ? -INFINITY : (float)(p.r + log_s);
-        if (a.entropy) a.entropy[i] = bad ? NAN : none ? 0.0f : (float)(log_s - p.e / p.s);
+        if (a.entropy) a.entropy[i] = bad ? NAN : none ? 0.0f : (float)fmax(log_s - p.e / p.s, 0.0);
         if (a.logp) a.logp[i] = l.label < 0 ? 0.0f : (uint64_t)l.label >= a.classes ? NAN : log_prob(value_of(l.logit, a.fl));
     }
     if (thread < a.topk) {
@@ -538,16 +541,16 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
 
     const LabelOf<T> wanted(a, i, row);
     const float to_log2 = 1.44269504f * ldexpf(1.0f, -a.fl);
-    V r = FIXED ? (V)0 : kFloat ? (V)-INFINITY : (V)INT32_MIN;
+    V r = 0;
     bool begun = FIXED;
     double s = 0.0, e = 0.0;
     int bad = 0;
     // a reference for values up to `largest`; false: nothing to add
     const auto refer = [&](V largest) -> bool {
-        if (kFloat && !(largest < (V)INFINITY)) { bad = 1; return false; }
+        if (kFloat && !((float)largest < INFINITY)) { bad = 1; return false; }
         if (FIXED) return true;
         const float ahead = begun ? (float)((double)largest - (double)r) * to_log2 : INFINITY;
-        if (ahead > 11.5f && (!kFloat || largest > (V)-INFINITY)) {
+        if (ahead > 11.5f && (!kFloat || (float)largest > -INFINITY)) {
             const double d = ((double)r - (double)largest) * (double)to_log2, k = begun ? exp2(d) : 0.0;
             e = begun ? k * (e + d * s) : 0.0;
             s *= k;
@@ -566,7 +569,10 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
     V largest = 0;
     uint32_t where = ~0u;
     const uint32_t edge_unit = threadIdx.x < head ? 0 : 0x7ffffff0u;
-    const auto clean = [](V v) -> V { return v != v ? (V)-INFINITY : v; };      // fp32 only
+    const auto clean = [](V v) -> V {
+        if constexpr (kFloat) return v != v ? -INFINITY : v;
+        else return v;
+    };
     V edge = 0;
     if (on_edge) {
         edge = (V)row[edge_col];
@@ -910,17 +916,16 @@ static void for_slabs(LogitArgs a, uint64_t rows_per_block, const Launch &launch
 }
 
 template <typename T>
-static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsPlan &p, int wl)
+static void launch_log_probs(adapt_ctx *ctx, const LogitArgs &a, const LogProbsPlan &p)
 {
-    const int span = sizeof(T) == 4 ? wl : 8 * (int)sizeof(T);
-    const bool fixed = !__is_same(T, float) && span - 1 - a.fl <= 4;
+    const bool fixed = sizeof(T) == 1 && a.fl >= 3;
     LogChunkArgs c = {p.splits, p.units, reinterpret_cast<LogPart *>(scratch(ctx)), reinterpret_cast<uint64_t *>(scratch(ctx) + p.part_bytes),
                       (int)(4 * p.threads)};
     const dim3 block(p.threads);
     const size_t lds = a.topk > 0 ? c.listed * sizeof(uint64_t) : 0;
     for_slabs(a, 1, [&](const LogitArgs &s, unsigned rows) {
         const dim3 grid(rows * p.splits);
-        if constexpr (!__is_same(T, float)) {
+        if constexpr (sizeof(T) == 1) {
             if (fixed && a.topk > 0) hipLaunchKernelGGL((log_probs_kernel<T, true, true>), grid, block, lds, ctx->stream, s, c);
             else if (fixed) hipLaunchKernelGGL((log_probs_kernel<T, false, true>), grid, block, lds, ctx->stream, s, c);
         }
@@ -962,10 +967,10 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     }
     const LogProbsPlan p = plan_log_probs(ctx->num_cu, rows, classes, topk, f);
     if (p.ws_bytes > scratch_bytes(ctx)) return ADAPT_EWORKSPACE;
-    if (f.wl == ADAPT_WL_FP32) launch_log_probs<float>(ctx, a, p, f.wl);
-    else if (f.wl <= 8) launch_log_probs<int8_t>(ctx, a, p, f.wl);
-    else if (f.wl <= 16) launch_log_probs<int16_t>(ctx, a, p, f.wl);
-    else launch_log_probs<int32_t>(ctx, a, p, f.wl);
+    if (f.wl == ADAPT_WL_FP32) launch_log_probs<float>(ctx, a, p);
+    else if (f.wl <= 8) launch_log_probs<int8_t>(ctx, a, p);
+    else if (f.wl <= 16) launch_log_probs<int16_t>(ctx, a, p);
+    else launch_log_probs<int32_t>(ctx, a, p);
     return hip_status(ctx, hipGetLastError());
 }
 
