@@ -32,22 +32,22 @@ __device__ __forceinline__ long long code_at(const void *q, int es, uint64_t i)
     return es == 1 ? static_cast<const int8_t *>(q)[i] : es == 2 ? static_cast<const int16_t *>(q)[i] : static_cast<const int32_t *>(q)[i];
 }
 
-// |X| <= 2^62 (x has 32 bits, up <= 31) and |res 2^res_up| <= 2^62, the positive ends left out: the sum fits 64 bits
+// |X| <= 2^62 (x has 32 bits, 0 <= up <= 31) and |res 2^res_up| <= 2^62, the positive ends left out: the sum fits 64 bits
 __device__ __forceinline__ long long drop_one(long long x, int up, int drop, int keep, uint32_t r16, int mode)
 {
     if ((int)r16 < drop) return 0;
-    const long long X = up >= 0 ? (long long)((unsigned long long)x << up) : x >> -up;
+    const long long X = (long long)((unsigned long long)x << up);
     const long long t = X + (mode == ADAPT_SR ? (int)r16 - drop : keep >> 1);
     const long long q = t / keep;
     return q - (q * keep > t);                             // towards minus infinity
 }
 
-// What bounds it: 8-bit codes the vector units (a Philox block is 19 64-bit products and 20 three-way xors for 8 elements, 12 of
-// about 18 instruction slots each), wider ones memory.  33.5 M codes, us: 8 -> 8 bits 16.4 (4.1 TB/s), with an 8-bit residual
-// 24.6 (4.1), 16 -> 16 bits 27.1 (4.95; a copy on this card runs at 5.0).
+// What bounds it: the issue of vector instructions at 8 bits (about 11 per element, 5 of them the generator's 19 products and 20 three-way
+// xors per block of eight; 4 more with a residual), memory above.  33.5 M codes, us: 8 -> 8 bits 15.8 (4.2 TB/s), with an 8-bit residual
+// 22 to 25 (4.0 to 4.5), 16 -> 16 bits 27 (4.95; a copy on this card runs at 5.0).
 //
-// How floor((X + u)/K) is found; all of them exactly.  33.5 M codes of 8 bits, us: BY_TABLE 16.4, BY_F64 28.2; of 16 bits:
-// BY_I32 27.1, BY_F64 34.2.  The faster form is taken wherever it is exact.
+// How floor((X + u)/K) is found; all of them exactly.  33.5 M codes of 8 bits, us: BY_TABLE 15.8, BY_F64 28; of 16 bits:
+// BY_I32 27, BY_F64 34.  The faster form is taken wherever it is exact; 64-bit integers (8.4 M codes of 32 bits 50, BY_F64 12) where none is.
 //   BY_TABLE  8-bit x: the quotient and the rest of X/K for each of its 256 values, in LDS.  An entry is q 2^16 + r with r + R
 //             carrying into the quotient where R is among the r largest draws, so that adding R to it rounds.
 //   BY_I32    |X + u| < 2^31, K >= 2^11: an fp32 quotient is off by less than one, and the rest says by what.
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a,
             out[i] = (TO)one(x[i], has_res ? (int)code_at(a.res, a.es_res, i) : 0, rounding_bits_of(a.seed, a.stream, i, ADAPT_SR));
 }
 
-// X beyond 2^50: 64-bit integers
+// X beyond 2^50: 64-bit integers, an element per thread
 __global__ void __launch_bounds__(kDropThreads) dropout_i64_kernel(const DropArgs a)
 {
     const long long hi = (1ll << (a.wl - 1)) - 1, lo = -hi - 1;
