@@ -137,3 +137,17 @@ def test_refusals():
         c.dropout(x, (8, 4), 0.5, res=x[:32], fres=(8, 4))
     with pytest.raises(ValueError):
         c.dropout(x, (8, 4), 0.5, out=torch.zeros(64, dtype=torch.int16, device="cuda"))
+
+
+def test_more_elements_than_32_bits_count():
+    n, tail = (1 << 32) + 1003, 5001
+    rng = np.random.default_rng(5)
+    last = _codes(rng, tail, 8)
+    x = torch.ones(n, dtype=torch.int8, device="cuda")
+    x[-tail:] = dev(last)
+    out = ctx().dropout(x, (8, 4), 0.25, seed=8, stream=9)
+    from oracle import fxp_oracle as orc
+    bits = orc.rounding_bits(tail, orc.SR, 8, 9, start=n - tail)
+    assert np.array_equal(host(out[-tail:]), head.dropout_with_bits(last, 4, 0.25, 8, 4, bits))
+    bits = orc.rounding_bits(4096, orc.SR, 8, 9)
+    assert np.array_equal(host(out[:4096]), head.dropout_with_bits(np.ones(4096), 4, 0.25, 8, 4, bits))

@@ -390,3 +390,25 @@ def test_fewer_chunks_than_alternatives(wl):
     y = _labels(rng, rows, classes)
     _check_log_probs(x, (wl, _fl(wl)) if wl else None, y, 32)
     _check_cross_entropy(x[:3], (wl, _fl(wl)) if wl else None, y[:3], (8, 7))
+
+
+def test_more_elements_than_32_bits_count():
+    """The draws of rows that lie behind the first 2^32 elements; all rows but the last ones have no label."""
+    rows, classes = 65560, 65537
+    x = torch.zeros((rows, classes), dtype=torch.int8, device="cuda")
+    rng = np.random.default_rng(4)
+    last = _logits(rng, 3, classes, 8, 4)
+    x[-3:] = dev(last)
+    y = torch.full((rows,), -1, dtype=torch.int64, device="cuda")
+    labels = np.array([5, 65536, 40000])
+    y[-3:] = dev(labels)
+    dl, logp = ctx().cross_entropy(x, (8, 4), y, (8, 7), seed=6, stream=7)
+    g = head.gradient(last, 4, labels)
+    lim = np.longdouble(128)
+    t = np.floor(np.clip(g * lim, -lim, lim - 1) * 65536).astype(np.int64).ravel()
+    want = np.minimum((t + orc.rounding_bits(t.size, orc.SR, 6, 7, start=(rows - 3) * classes)) >> 16, 127)
+    assert np.array_equal(host(dl[-3:]).ravel(), want)
+    assert not dl[-4].any() and not dl[0].any() and not logp[:-3].any()
+    r = ctx().log_probs(x, (8, 4), y, topk=1)
+    assert torch.equal(r["top_idx"][:-3], torch.zeros_like(r["top_idx"][:-3]))
+    assert np.array_equal(host(r["top_idx"][-3:])[:, 0], last.argmax(1))
