@@ -791,15 +791,17 @@ class Context:
         labels), lse, entropy (None unless asked for), top_idx int32[rows, topk], top_logp (None if topk = 0))."""
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
-        lse = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        # one allocation for what has a value per row: rows of it cost half of what tensors of their own do
+        per_row = torch.empty(1 + (labels is not None) + bool(entropy), rows, dtype=torch.float32, device=logits.device).unbind()
+        lse = per_row[0]
         logp = ent = idx = top = label_at = logp_at = ent_at = idx_at = top_at = None
         if labels is not None:
             if not self._dense(labels, torch.int64) or labels.shape != lse.shape:
                 self._own("labels", labels, torch.int64, (rows,))
-            logp = torch.empty_like(lse)
+            logp = per_row[1]
             label_at, logp_at = labels.data_ptr(), logp.data_ptr()
         if entropy:
-            ent = torch.empty_like(lse)
+            ent = per_row[-1]
             ent_at = ent.data_ptr()
         if topk > 0:
             top = torch.empty((rows, topk), dtype=torch.float32, device=logits.device)

@@ -877,7 +877,7 @@ static CrossEntropyPlan plan_cross_entropy(int num_cu, uint64_t rows, uint64_t c
     CrossEntropyPlan p = {};
     const uint64_t all = std::max<uint64_t>(classes / U, 1), wanted = 4 * (uint64_t)num_cu /* blocks */;
     uint64_t splits = 1;
-    if (rows > 0 && rows * 2 <= (uint64_t)num_cu && all >= 3072) splits = std::min<uint64_t>((wanted + rows - 1) / rows, all / 256);
+    if (rows > 0 && rows * 2 <= (uint64_t)num_cu && all >= 3200) splits = std::min<uint64_t>((wanted + rows - 1) / rows, all / 256);
     p.splits = (uint32_t)splits;
     p.units = (uint32_t)((all + splits - 1) / splits);
     const bool alone = rows <= (uint64_t)num_cu;
