@@ -468,14 +468,14 @@ __device__ __forceinline__ void one_by_one(int k, TopScratch &s, const Every &ev
     }
 }
 
-// a row's label and its logit, loaded before they are needed
+// a row's label and its logit, each loaded before it is needed
 template <typename T>
 struct LabelOf {
-    int64_t label = -1;
+    int64_t label;
     T logit = 0;
-    __device__ __forceinline__ LabelOf(const LogitArgs &a, uint64_t i, const T *row)
+    __device__ __forceinline__ LabelOf(const LogitArgs &a, uint64_t i) : label(a.logp ? a.labels[i] : -1) {}
+    __device__ __forceinline__ void look_up(const LogitArgs &a, const T *row)
     {
-        if (a.logp) label = a.labels[i];
         if (label >= 0 && (uint64_t)label < a.classes) logit = row[label];
     }
 };
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
     const bool on_edge = chunk == 0 && threadIdx.x < head + tail;
     const uint32_t edge_col = threadIdx.x < head ? threadIdx.x : (uint32_t)a.classes - (head + tail) + threadIdx.x;
 
-    const LabelOf<T> wanted(a, i, row);
+    LabelOf<T> wanted(a, i);
     const float to_log2 = 1.44269504f * ldexpf(1.0f, -a.fl);
     V r = 0;
     bool begun = FIXED;
@@ -615,6 +615,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
         }
     }
     if (TOP && on_edge && (where == ~0u || (edge_unit == 0 ? edge >= largest : edge > largest))) { largest = edge; where = edge_unit; }
+    if (c.splits == 1) wanted.look_up(a, row);
     // one reference for the block
     const auto maximum = [](double x, double y) { return fmax(x, y); };
     const double ln2 = 0.69314718055994530942;
@@ -711,8 +712,9 @@ __global__ void __launch_bounds__(kSmallThreads) log_probs_small_kernel(const Lo
     if (i >= a.rows) return;
     const int lane = threadIdx.x & (kWave - 1), classes = (int)a.classes;
     const T *row = static_cast<const T *>(a.logits) + i * a.ld;
-    const LabelOf<T> wanted(a, i, row);
+    LabelOf<T> wanted(a, i);
     const SmallRow<T> x(row, classes, a.fl);
+    wanted.look_up(a, row);
     LogPart p = {x.m, 0.0, 0.0};
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -783,17 +785,27 @@ __global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const Logi
     __shared__ double part_r[kMostThreads / kWave];
     __shared__ Pair part_s[kMostThreads / kWave];
     const uint64_t i = blockIdx.x;
-    const LabelOf<T> wanted(a, i, static_cast<const T *>(a.logits) + i * a.ld);
+    LabelOf<T> wanted(a, i);
     const LogPart *parts = c.part + i * c.splits;
-    double ref = -INFINITY;
-    int bad = 0;
-    for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) {
+    // a chunk's keys are in order: it is taken in `slices` of every so many, so that there are 64 largest ones to compare
+    const uint64_t *keys = c.keys + i * c.splits * a.topk;
+    const uint32_t slices = min((uint32_t)a.topk, (kWave + c.splits - 1) / c.splits), heads = c.splits * slices;
+    const auto head_of = [&](uint32_t j) { return keys + (uint64_t)(j / slices) * a.topk + j % slices; };
+    // everything that has to come from memory first
+    const LogPart none = {-INFINITY, 0.0, 0.0}, own = threadIdx.x < c.splits ? parts[threadIdx.x] : none;
+    uint64_t mine = 0;
+    for (uint32_t j = threadIdx.x; j < heads; j += kJoinThreads) mine = max(mine, *head_of(j));
+    wanted.look_up(a, static_cast<const T *>(a.logits) + i * a.ld);
+    double ref = own.r;
+    int bad = own.r != own.r;
+    for (uint32_t j = threadIdx.x + kJoinThreads; j < c.splits; j += kJoinThreads) {
         ref = fmax(ref, parts[j].r);
         bad |= parts[j].r != parts[j].r;
     }
     ref = over_block(ref, part_r, [](double x, double y) { return fmax(x, y); });
-    LogPart p = {ref, 0.0, 0.0};
-    for (uint32_t j = threadIdx.x; j < c.splits; j += kJoinThreads) {
+    LogPart p = own;
+    rebase(p, ref);
+    for (uint32_t j = threadIdx.x + kJoinThreads; j < c.splits; j += kJoinThreads) {
         LogPart q = parts[j];
         rebase(q, ref);
         p.s += q.s;
@@ -804,12 +816,6 @@ __global__ void __launch_bounds__(kJoinThreads) join_log_probs_kernel(const Logi
     p.e = sums.b;
     if (__syncthreads_or(bad)) p.r = NAN;
     if (a.topk > 0) {
-        // a chunk's keys are in order: it is taken in `slices` of every so many, so that there are 64 largest ones to compare
-        const uint64_t *keys = c.keys + i * c.splits * a.topk;
-        const uint32_t slices = min((uint32_t)a.topk, (kWave + c.splits - 1) / c.splits), heads = c.splits * slices;
-        const auto head_of = [&](uint32_t j) { return keys + (uint64_t)(j / slices) * a.topk + j % slices; };
-        uint64_t mine = 0;
-        for (uint32_t j = threadIdx.x; j < heads; j += kJoinThreads) mine = max(mine, *head_of(j));
         const uint64_t bound = bound_of(mine, a.topk, top, list);
         if (mine >= bound)
             for (uint32_t j = threadIdx.x; j < heads; j += kJoinThreads) {
