@@ -74,10 +74,11 @@ __device__ __forceinline__ T unit_get(const uint32_t (&w)[kWords<T>], int e)
 }
 
 // exp in fp64 of a number of at most 700: 2^(n/256) e^r, |r| <= ln 2 / 512, with a table of the 256 roots and four terms (the
-// next is 4e-17).  Below -700 the result is some number below 1e-300.
+// next is 4e-17).  It ends as fp64 does: subnormal below -708, 0 below -745.2 and for -inf (a class of p = 0 has a gradient of 0, and
+// not of a little below 0 under a negative weight).
 __device__ __forceinline__ double exp_by_roots(double d, const double *roots)
 {
-    d = fmax(d, -700.0);
+    d = fmax(d, -800.0);
     const double shifted = fma(d, 369.32993046757462711, 6755399441055744.0);      // 256 / ln 2; 1.5 2^52 leaves n in the low word
     const int n = __double2loint(shifted);
     const double r = fma(shifted - 6755399441055744.0, -0.0027076061740622863, d); // ln 2 / 256
@@ -85,8 +86,7 @@ __device__ __forceinline__ double exp_by_roots(double d, const double *roots)
     p = fma(p, r, 0.5);
     p = fma(p, r, 1.0);
     p = fma(p, r, 1.0);
-    p *= roots[n & 255];
-    return __hiloint2double(__double2hiint(p) + ((n >> 8) << 20), __double2loint(p));
+    return ldexp(p * roots[n & 255], n >> 8);
 }
 
 // The exponentials of one type of logits relative to a reference, as each block sets them up in LDS.
