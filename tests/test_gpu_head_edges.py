@@ -5,6 +5,7 @@ import pytest
 from gpu_util import ctx, dev, host
 from oracle import fxp_oracle as orc
 from oracle import head_oracle as head
+from test_gpu_head import EPS, _fl, _logits, _near
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +26,32 @@ def test_masked_classes_have_no_gradient_whatever_the_weight(rows, classes, wl_g
     got = host(ctx().cross_entropy(dev(x), None, dev(y), (wl_g, wl_g - 1), weights=dev(w), seed=3, stream=5)[0])
     assert not got[masked].any()
     assert np.array_equal(got, head.quantize_real(head.gradient(x, None, y, w), wl_g, wl_g - 1, seed=3, stream=5))
+
+
+@pytest.mark.parametrize("rows,classes", [(9, 3), (9, 200), (9, 3000), (9, 70001)])
+def test_a_certain_class_has_the_logarithm_of_one(rows, classes):
+    x = np.full((rows, classes), -np.inf, dtype=np.float32)
+    y = (np.arange(rows) * 31) % classes
+    x[np.arange(rows), y] = np.linspace(-700, 700, rows)
+    assert not host(ctx().cross_entropy(dev(x), None, dev(y), (8, 7))[1]).any()
+    r = ctx().log_probs(dev(x), None, dev(y), topk=1)
+    assert not host(r["logp"]).any() and not host(r["top_logp"]).any() and not host(r["entropy"]).any()
+    assert np.array_equal(host(r["lse"]), x[np.arange(rows), y])
+
+
+@pytest.mark.parametrize("rows,classes", [(40, 100), (40, 2000), (200, 5001), (3, 60001)])
+@pytest.mark.parametrize("wl", [0, 8, 12, 16, 24])
+def test_the_loss_has_all_of_its_bits(rows, classes, wl):
+    """Sum and logarithm are in 64 bits: beside the rounding of the result there are only theirs, at most 2^11 additions
+    in a row (2^-42), exponentials and logarithm (2^-48 together)."""
+    rng = np.random.default_rng([rows, classes, wl])
+    x = _logits(rng, rows, classes, wl, _fl(wl))
+    y = rng.integers(0, classes, rows)
+    if wl == 0:
+        x[np.arange(rows), y] = rng.random(rows) * 30
+    else:
+        lim = (1 << (wl - 1)) - 1
+        x[np.arange(rows), y] = np.rint(lim * rng.random(rows)).astype(x.dtype)
+    logp = ctx().cross_entropy(dev(x), (wl, _fl(wl)) if wl else None, dev(y), (8, 7))[1]
+    want = head.log_probs(x, _fl(wl) if wl else None, y, 0)["logp"]
+    _near(host(logp), want, EPS * np.abs(want) + 2.0 ** -41, "logp")
