@@ -280,12 +280,13 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     if constexpr (MODE != CHUNK_CODES) {
         double s = 0.0;
         if constexpr (kFloat) {
-            // every thread has a reference of its own, which follows the logits only where they get 600 ahead of it
+            // every thread has a reference of its own, which follows the logits only where they get 600 ahead of it (the difference
+            // is exact to half a step of its own; r + 600 may lie hundreds further on, where exponentials end)
             float r = -INFINITY;
             int bad = 0;
             const auto take = [&](float largest) -> bool {
                 if (!(largest < INFINITY)) { bad = 1; return false; }
-                if (largest > r + 600.0f) { s = r > -INFINITY ? s * exp((double)r - (double)largest) : 0.0; r = largest; }
+                if (largest - r > 600.0f) { s = r > -INFINITY ? s * exp((double)r - (double)largest) : 0.0; r = largest; }
                 return largest > -INFINITY;
             };
             if (on_edge && take(edge)) s += ex.at(edge, r);

@@ -28,6 +28,22 @@ def test_masked_classes_have_no_gradient_whatever_the_weight(rows, classes, wl_g
     assert np.array_equal(got, head.quantize_real(head.gradient(x, None, y, w), wl_g, wl_g - 1, seed=3, stream=5))
 
 
+@pytest.mark.parametrize("at", [1e10, -1e10, 2.0 ** 33, -2.0 ** 33, 2.0 ** 34 - 4096, 2.0 ** 32, -3e9, 1e12])
+@pytest.mark.parametrize("rows,classes", [(3, 200), (3, 20000), (3, 60000)])
+def test_large_logits_one_step_apart(at, rows, classes):
+    """Logits whose neighbours in fp32 are 256 to 65536 apart: the larger ones share the row."""
+    x = np.full((rows, classes), at, dtype=np.float32)
+    up = np.nextafter(np.float32(at), np.float32(np.inf))
+    x[0, classes // 2::classes // 8] = up
+    x[1, -1] = up
+    y = np.array([classes // 2, classes - 1, 3])
+    got, logp = ctx().cross_entropy(dev(x), None, dev(y), (16, 15), seed=3, stream=5)
+    want = head.log_probs(x, None, y, 3)
+    _near(host(logp), want["logp"], EPS * np.abs(want["logp"]) + 2.0 ** -40, "logp")
+    assert np.array_equal(host(got), head.quantize_real(head.gradient(x, None, y), 16, 15, seed=3, stream=5))
+    assert np.array_equal(host(ctx().log_probs(dev(x), None, dev(y), topk=3)["top_idx"]), want["top_idx"])
+
+
 @pytest.mark.parametrize("rows,classes", [(9, 3), (9, 200), (9, 3000), (9, 70001)])
 def test_a_certain_class_has_the_logarithm_of_one(rows, classes):
     x = np.full((rows, classes), -np.inf, dtype=np.float32)
