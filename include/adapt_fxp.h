@@ -538,12 +538,12 @@ int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t n, double 
 #define ADAPT_WL_FP32 0
 
 /* Log probabilities of given classes, and the largest ones.
- *   logp     device float[rows] or NULL: x_i,label - lse_i; 0 for a row without label.  labels may
- *            be NULL if logp is
+ *   logp     device float[rows] or NULL: x_i,label - lse_i, at most 0; 0 for a row without label.
+ *            labels may be NULL if logp is
  *   lse      device float[rows] or NULL;  entropy  device float[rows] or NULL: -sum_j p_ij log p_ij
  *   topk     0..32, at most classes: top_index = device int32_t[rows*topk], the classes of the topk
  *            largest logits of each row, largest first, equal ones (and +0, -0) by their index; a NaN
- *            counts as -inf.  top_logp = device float[rows*topk], their log probabilities.  Both may
+ *            counts as -inf.  top_logp = device float[rows*topk], their log probabilities (at most 0).  Both may
  *            be NULL if topk is 0
  * Workspace: adapt_workspace_bytes with ADAPT_CALL_LOG_PROBS. */
 int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows, size_t classes,

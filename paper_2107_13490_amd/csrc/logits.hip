@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kMostThreads, 8) cross_entropy_kernel(const Lo
     }
 
     const bool bad = sum != sum, none = ref == -INFINITY;
-    if (tells) a.logp[i] = bad ? NAN : none ? -INFINITY : (float)(value_of(row[label], a.fl) - ref - log_of_sum(sum));
+    if (tells) a.logp[i] = bad ? NAN : none ? -INFINITY : (float)fmin(value_of(row[label], a.fl) - ref - log_of_sum(sum), 0.0);
     const double weight = a.weights ? (double)a.weights[i] : 1.0;
     if (bad || none || !(fabs(weight) < INFINITY)) {
         no_gradient();
@@ -516,7 +516,9 @@ __device__ __forceinline__ void finish_row(const LogitArgs &a, uint64_t i, const
 {
     const bool bad = p.r != p.r, none = p.r == -INFINITY;
     const double log_s = log_of_fp32_sum(p.s);
-    const auto log_prob = [&](double x) { return bad ? NAN : none ? -INFINITY : (float)(x - p.r - log_s); };
+    // at most 0, as the entropy is at least 0: exponents of up to 23 are rounded to fp32 (8-bit codes with the reference 0), so that a sum
+    // can be smaller than its largest term by 8e-7 of itself
+    const auto log_prob = [&](double x) { return bad ? NAN : none ? -INFINITY : (float)fmin(x - p.r - log_s, 0.0); };
     if (thread == 0) {
         if (a.lse) a.lse[i] = bad ? NAN : none ? -INFINITY : (float)(p.r + log_s);
         if (a.entropy) a.entropy[i] = bad ? NAN : none ? 0.0f : (float)fmax(log_s - p.e / p.s, 0.0);
@@ -785,7 +787,7 @@ __global__ void __launch_bounds__(kSmallThreads) cross_entropy_small_kernel(cons
     s = wave_sum(s);
     const bool counts = there && x.m > -INFINITY && fabs(weight) < INFINITY;
     if (lane == 0 && a.logp)
-        a.logp[i] = label < 0 ? 0.0f : !there || x.m != x.m ? NAN : x.m == -INFINITY ? -INFINITY : (float)(at_label - x.m - log_of_sum(s));
+        a.logp[i] = label < 0 ? 0.0f : !there || x.m != x.m ? NAN : x.m == -INFINITY ? -INFINITY : (float)fmin(at_label - x.m - log_of_sum(s), 0.0);
     const double tmin = -ldexp(1.0, a.wl_g + 15), tmax = ldexp(1.0, a.wl_g + 15) - 65536.0, scale = weight * ldexp(1.0, a.fl_g + 16) / s;
     G *grad = static_cast<G *>(a.grad) + i * a.ldg;
 #pragma unroll

@@ -44,6 +44,25 @@ def test_large_logits_one_step_apart(at, rows, classes):
     assert np.array_equal(host(ctx().log_probs(dev(x), None, dev(y), topk=3)["top_idx"]), want["top_idx"])
 
 
+@pytest.mark.parametrize("rows,classes", [(127, 10), (127, 300), (127, 5000), (60, 200003)])
+@pytest.mark.parametrize("f", [(8, 3), (8, 4), (8, 1), (12, 7), (16, 8), (24, 18), None])
+def test_probabilities_are_at_most_one(rows, classes, f):
+    """Rows with one class that has nearly all of it: its log probability is rounded to 0 at most."""
+    c = np.arange(1, rows + 1)
+    y = (c * 7919) % classes
+    if f is None:
+        x = np.full((rows, classes), -40, dtype=np.float32)
+        x[np.arange(rows), y] = c / 8 + 0.1
+    else:
+        x = np.full((rows, classes), -(1 << (f[0] - 1)), dtype=np.int8 if f[0] <= 8 else np.int16 if f[0] <= 16 else np.int32)
+        x[np.arange(rows), y] = c * 2 ** (f[0] - 8)
+    r = ctx().log_probs(dev(x), f, dev(y), topk=2)
+    logp = host(ctx().cross_entropy(dev(x), f, dev(y), (8, 7))[1])
+    for v in (host(r["logp"]), host(r["top_logp"]), logp):
+        assert v.max() <= 0, v.max()
+    assert np.array_equal(host(r["top_idx"])[:, 0], y)
+
+
 @pytest.mark.parametrize("rows,classes", [(9, 3), (9, 200), (9, 3000), (9, 70001)])
 def test_a_certain_class_has_the_logarithm_of_one(rows, classes):
     x = np.full((rows, classes), -np.inf, dtype=np.float32)
