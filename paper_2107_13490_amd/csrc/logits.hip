@@ -1004,6 +1004,17 @@ extern "C" int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, 
     return hip_status(ctx, hipGetLastError());
 }
 
+// The reference of integer logits where it is the largest code: of the storage for int16 (distances to it index tables), of the format for
+// int32.  (8-bit codes take 0, fp32 logits what the rows hold.)
+struct FixedReference { bool fixed; int top; };
+template <typename T>
+static FixedReference fixed_reference(int wl, int fl)
+{
+    if (sizeof(T) == 1 || __is_same(T, float)) return {false, 0};
+    const int span = sizeof(T) == 2 ? 16 : wl;
+    return {span - fl <= 9, (int)((1ll << (span - 1)) - 1)};
+}
+
 template <typename T, typename G>
 static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
 {
@@ -1011,15 +1022,14 @@ static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const Cross
     // caches / past them, alone and with a copy of the codes behind: 62 MiB (2048 x 32000, 8 bits) 33.5 / 33.4, 51 / 57; 125 MiB (4096)
     // 74 / 60, 127 / 123; 128 MiB (1024 x 65531, 16 bits) 83 / 66, 133 / 126; 250 MiB (8192 x 32000, 8 bits) 134 / 127, 231 / 229
     const bool past = a.rows * a.classes * sizeof(G) >= ((uint64_t)96 << 20);
-    // distances to the largest code: of the storage for int16 (they index tables), of the format for int32
-    const int span = sizeof(T) == 2 ? 16 : wl;
     if (a.classes <= (uint64_t)kSmall) {
         for_slabs(a, kSmallThreads / kWave, [&](const LogitArgs &s, unsigned blocks) {
             hipLaunchKernelGGL((cross_entropy_small_kernel<T, G>), dim3(blocks), dim3(kSmallThreads), 0, ctx->stream, s);
         });
         return;
     }
-    const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), span - a.fl <= 9, (int)((1ll << (span - 1)) - 1), past};
+    const FixedReference ref = fixed_reference<T>(wl, a.fl);
+    const ChunkArgs c = {p.splits, p.units, reinterpret_cast<RowPart *>(scratch(ctx)), ref.fixed, ref.top, past};
     const dim3 block(p.threads);
     for_slabs(a, 1, [&](const LogitArgs &s, unsigned rows) {
         const dim3 grid(rows * p.splits);
