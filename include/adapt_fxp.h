@@ -556,7 +556,9 @@ int adapt_log_probs(adapt_ctx *ctx, const void *logits, adapt_fmt f, size_t rows
  *             quantize(weights_i (p_ij - [j = labels_i])) by adapt_quantize's rule for the real
  *             value (evaluated in 64 bits), with the random bits of element i*classes + j.
  *             0 in rows without label and, whatever the weight, for masked classes (as which logits count that are
- *             so far below the row's largest that their p vanishes in 64 bits).  Must not overlap the logits
+ *             so far below the row's largest that their p vanishes in 64 bits).  Must not share memory with
+ *             the logits, which are read until the last code is written (ADAPT_EINVAL); its rows may lie between
+ *             theirs where both are the same number of bytes apart
  *   weights   device float[rows], or NULL for 1 everywhere (a mean over the rows is a power of two in
  *             fg.fl and a weight).  A row whose weight is not finite has a gradient of 0
  * |p - [..]| <= 1, so fg.fl = fg.wl - 1 loses nothing but the code of exactly 1.

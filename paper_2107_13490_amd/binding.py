@@ -814,7 +814,8 @@ class Context:
     def cross_entropy(self, logits, f, labels, fg, weights=None, mode=SR, seed=0, stream=0, out=None):
         """Softmax cross entropy of `logits` (as for log_probs) against labels (int64[rows], negative: row left out), rows
         weighted by weights (fp32[rows] or None).  Returns (dlogits, logp): the gradient weights (p - onehot) as codes of
-        format fg = (wl, fl), what Net.backward takes with dlogits_fl = fl, and the labels' log probabilities."""
+        format fg = (wl, fl), what Net.backward takes with dlogits_fl = fl, and the labels' log probabilities.  out, if given,
+        must not share memory with the logits (an error)."""
         torch = self._torch
         f, rows, classes, ld = self._logits(logits, f)
         fg = _fmt(fg)

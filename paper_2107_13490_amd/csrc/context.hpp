@@ -96,6 +96,18 @@ inline uint32_t *ticket(adapt_ctx *c, int slot) { return reinterpret_cast<uint32
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned_to(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 
+// Whether `rows` rows of bytes_a bytes, pitch_a apart, share memory with as many rows of bytes_b bytes, pitch_b apart.  Rows that lie
+// between each other's are told apart where both are equally far apart; otherwise everything between the first and the last byte counts.
+inline bool rows_overlap(const void *a, uint64_t bytes_a, uint64_t pitch_a, const void *b, uint64_t bytes_b, uint64_t pitch_b, uint64_t rows)
+{
+    const uintptr_t at_a = reinterpret_cast<uintptr_t>(a), at_b = reinterpret_cast<uintptr_t>(b);
+    if (at_b >= at_a + (rows - 1) * pitch_a + bytes_a || at_a >= at_b + (rows - 1) * pitch_b + bytes_b) return false;
+    if (rows == 1 || pitch_a != pitch_b) return true;
+    // b's rows start this far behind the starts of a's
+    const uint64_t behind = at_b >= at_a ? (at_b - at_a) % pitch_a : (pitch_a - (at_a - at_b) % pitch_a) % pitch_a;
+    return behind < bytes_a || behind + bytes_b > pitch_a;
+}
+
 // the device that the context was created on is the one that a launch would go to now
 inline bool on_current_device(const adapt_ctx *c)
 {

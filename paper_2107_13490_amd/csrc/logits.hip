@@ -1060,6 +1060,9 @@ extern "C" int adapt_cross_entropy(adapt_ctx *ctx, const void *logits, adapt_fmt
     if (!logits || !labels || !dlogits || !aligned_to(logits, logit_bytes(f)) || !aligned_to(labels, 8) || !aligned_to(weights, 4) ||
         !aligned_to(dlogits, storage_bytes(fg)) || !aligned_to(logp, 4))
         return ADAPT_EINVAL;
+    // the codes are written while the row is still read
+    const uint64_t es = logit_bytes(f), es_g = storage_bytes(fg);
+    if (rows_overlap(logits, classes * es, ld * es, dlogits, classes * es_g, ldg * es_g, rows)) return ADAPT_EINVAL;
     LogitArgs a = {};
     a.logits = logits;
     a.rows = rows; a.classes = classes; a.ld = ld;

@@ -1,7 +1,9 @@
 """Log probabilities and cross entropy at the ends of their ranges, on the GPU against the oracle."""
 import numpy as np
 import pytest
+import torch
 
+import paper_2107_13490_amd as pkg
 from gpu_util import ctx, dev, host
 from oracle import fxp_oracle as orc
 from oracle import head_oracle as head
@@ -90,3 +92,19 @@ def test_the_loss_has_all_of_its_bits(rows, classes, wl):
     logp = ctx().cross_entropy(dev(x), (wl, _fl(wl)) if wl else None, dev(y), (8, 7))[1]
     want = head.log_probs(x, _fl(wl) if wl else None, y, 0)["logp"]
     _near(host(logp), want, EPS * np.abs(want) + 2.0 ** -41, "logp")
+
+
+def test_gradients_beside_the_logits_but_not_in_their_place():
+    rng = np.random.default_rng(2)
+    x, y = _logits(rng, 6, 300, 8, 4), rng.integers(0, 300, 6)
+    both = torch.zeros((6, 640), dtype=torch.int8, device="cuda")
+    both[:, 20:320] = dev(x)
+    t = both[:, 20:320]
+    for out in (t, both[:, 21:321], both[:, :300], both[:, 319:619]):
+        with pytest.raises(pkg.AdaptError):
+            ctx().cross_entropy(t, (8, 4), dev(y), (8, 7), out=out)
+    assert np.array_equal(host(t), x)
+    ctx().cross_entropy(t, (8, 4), dev(y), (8, 7), seed=1, stream=2, out=both[:, 320:620])
+    both = host(both)
+    assert np.array_equal(both[:, 20:320], x) and not both[:, :20].any() and not both[:, 620:].any()
+    assert np.array_equal(both[:, 320:620], head.quantize_real(head.gradient(x, 4, y), 8, 7, seed=1, stream=2))
