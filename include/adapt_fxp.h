@@ -518,7 +518,7 @@ int adapt_grad_add(adapt_ctx *ctx, const void *a, int wl_a, const int64_t *e_a, 
  * draws is exactly X 2^-16.
  * The gradient is the same call on the gradient's codes, with the same p, seed and stream.
  *   x    device, n codes of format fx (wl up to 32);  out  device, n codes of format fo; may be x or res
- *        where that has codes of the same size
+ *        where that has codes of the same size, and must not share memory with them otherwise (ADAPT_EINVAL)
  *   res  device, n codes of format fres that are added, or NULL (fres is then ignored)
  * 0 <= p, T <= 65535; n <= 2^40.  ADAPT_EUNSUPPORTED: fo.fl - fx.fl > 15, or fres.fl > fo.fl (the
  * residual is added as it is, not rounded). */

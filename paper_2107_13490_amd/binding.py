@@ -755,7 +755,8 @@ class Context:
     def dropout(self, x, fx, p, fo=None, res=None, fres=None, mode=SR, seed=0, stream=0, out=None):
         """Codes of format fx = (wl, fl) dropped with probability p and scaled by its counterpart, as codes of format fo
         (default: fx), plus the codes `res` of format fres.  The gradient is the same call on the gradient's codes, with
-        the same p, seed and stream; mode is the rounding of the kept ones."""
+        the same p, seed and stream; mode is the rounding of the kept ones.  out, if given, may be x or res where the codes
+        have one size, and must not share memory with them otherwise (an error)."""
         fx = _fmt(fx)
         fo = fx if fo is None else _fmt(fo)
         codes = self._codes

@@ -186,6 +186,9 @@ extern "C" int adapt_dropout(adapt_ctx *ctx, const void *x, adapt_fmt fx, size_t
     if (n == 0) return ADAPT_OK;
     const int es_x = storage_bytes(fx), es_o = storage_bytes(fo), es_r = res ? storage_bytes(fres) : 1;
     if (!x || !out || !aligned_to(x, es_x) || !aligned_to(out, es_o) || !aligned_to(res, es_r)) return ADAPT_EINVAL;
+    // a code may take the place of the one that it is made of, and of no other
+    const auto in_the_way = [&](const void *in, int es) { return !(in == out && es == es_o) && rows_overlap(in, n * es, 0, out, n * es_o, 0, 1); };
+    if (in_the_way(x, es_x) || (res && in_the_way(res, es_r))) return ADAPT_EINVAL;
     const int up = 16 + fo.fl - fx.fl, keep = 65536 - drop;
     const DropArgs a = {x, res, out, n, up, res ? fo.fl - fres.fl : 0, drop, keep, es_x, es_r, es_o, fo.wl, rng.mode, rng.seed, rng.stream};
     const bool nearest = rng.mode != ADAPT_SR;

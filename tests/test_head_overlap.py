@@ -55,3 +55,34 @@ def test_gradients_in_the_place_of_the_logits_are_refused(tmp_path):
             apart = d >= last or d + (rows - 1) * ldg * _bytes(wl_g) + classes * _bytes(wl_g) <= first
             assert status == (0 if apart else -1), c
     assert launches == got.count(0)
+
+
+DROPOUT = """
+h = context()
+for out, wl_x, wl_o, res, wl_res, n in calls:
+    F = b.Fmt
+    print(lib.adapt_dropout(h, at, F(wl_x, 4), n, 0.5, F(wl_o, 4), b.Rng(1, 1, 1), at + res if res is not None else None, F(wl_res, 4), at + out))
+print(len(fake.fake_launched().split()))
+"""
+
+
+def test_dropout_in_place_is_taken_and_in_part_of_the_place_refused(tmp_path):
+    """out may be x, or res, where the codes have one size (each is read before its successor is written); at any other distance
+    codes would be overwritten before they are read."""
+    def share(a, bytes_a, b, bytes_b):
+        return a < b + bytes_b and b < a + bytes_a
+
+    calls, want = [], []
+    for wl_x, wl_o, wl_res in itertools.product((8, 16, 32), repeat=3):
+        x, o, r = _bytes(wl_x), _bytes(wl_o), _bytes(wl_res)
+        for n in (1, 100):
+            for res in (None, 0, 4 * n, 1 << 20):
+                for out in (0, o, -o, 4, -4, 4 * n, n * x // o * o, -n * o, 8 * n, (1 << 20) + o, 1 << 20):
+                    calls.append((out, wl_x, wl_o, res, wl_res, n))
+                    bad = share(0, n * x, out, n * o) and not (out == 0 and x == o)
+                    if res is not None:
+                        bad = bad or (share(res, n * r, out, n * o) and not (out == res and r == o))
+                    want.append(-1 if bad else 0)
+    got, launches = _statuses(calls, tmp_path, DROPOUT)
+    assert got == want, next((c, g, w) for c, g, w in zip(calls, got, want) if g != w)
+    assert 0 < launches == want.count(0) < len(want)
