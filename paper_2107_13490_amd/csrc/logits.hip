@@ -80,7 +80,7 @@ __device__ __forceinline__ double log_of_sum(double s)
 // What bounds it: the two sweeps and the codes in memory, and at 8 bits as much the issue of 13 instructions per element, 5 of them the
 // generator's.  The rows in flight exceed an XCD's L2, so the second sweep comes from memory as well; rows kept in LDS or registers
 // leave too few wavefronts (8192 x 32000 of 8 bits 126 -> 131 us, 2047 x 65531 of 16 bits 143 -> 162).  us (TB/s of both sweeps and the
-// codes): 8192 x 32000, 8 -> 8 bits 123 (6.4), 1535 x 65531, 16 -> 16 bits 118 (5.7), 1024 x 50001, fp32 -> 8 bits 87 (5.2); a copy runs at 5.0.
+// codes): 8192 x 32000, 8 -> 8 bits 123 (6.4), 1535 x 65531, 16 -> 16 bits 118 (5.7), 922 of 1024 x 50001, fp32 -> 8 bits 87 (4.8); a copy runs at 5.0.
 // ---------------------------------------------------------------------------------------------
 template <typename T> constexpr int kUnit = sizeof(T) == 1 ? 16 : 8;      // elements
 template <typename T> constexpr int kWords = kUnit<T> * (int)sizeof(T) / 4;
@@ -695,8 +695,9 @@ __global__ void __launch_bounds__(kMostThreads, 8) log_probs_kernel(const LogitA
 }
 
 // Rows of up to kSmall classes: a wavefront each, whose lanes hold their logits.  us in a captured graph, this / a block per row:
-// 256 x 100 log probabilities of 8 bits 3.0 / 3.1, with 5 alternatives 4.7 / 8.2, cross entropy 4.0 / 5.0; 8192 x 100 5.1 / 6.0, 9.6 / 24,
-// 8.2 / 12.8.  At 256 classes (8192 rows) they meet: 5.9 / 5.9, 10.7 / 23, 11.5 / 11.7.
+// 256 x 100 log probabilities of 8 bits 3.1 / 3.2, with 5 alternatives 4.8 / 9.3, cross entropy 3.8 / 5.0; 8192 x 100 5.4 / 6.4, 10.0 / 27,
+// 7.7 / 12.3.  At 256 classes (8192 rows) they meet without alternatives, 6.1 / 6.3 and 11.1 / 11.3; with 5 of them (10.9 / 26) a wavefront
+// would be faster for longer rows, too.
 constexpr int kSmall = 256, kSmallThreads = 256;
 
 template <typename T>
@@ -863,9 +864,10 @@ struct LogProbsPlan {
 
 // Threads: a thread takes two units where blocks are few (eight where they fill the card), rows of 4096 units 1024 threads where each has a
 // compute unit of its own.  Chunks: a second launch and its join pay only for few, long rows.  us in a captured graph, chunks / a
-// block per row: 1 x 100000 of 8 bits (6250 units) 6.9 / 8.0, 16 bits with 8 alternatives (12500) 12.4 / 12.3, fp32 with 32 17.1 / 17.5;
-// 1 x 200000 6.9 / 12.7, 12.5 / 18.2, 17.1 / 24.6; 64 x 100000 8.7 / 8.6, 15.3 / 13.0, 23.1 / 18.0; 64 x 200000 9.5 / 13.2, 17.2 / 19.1,
-// 25.9 / 28.6; 200 x 200000 17.3 / 15.5, 29.3 / 21.6, 49.5 / 33.9.
+// block per row, 8 bits without alternatives, 16 bits with 8, fp32 with 32: 1 x 100000 (6250 or 12500 units) 6.0 / 7.9, 12.4 / 14.7,
+// 16.7 / 17.6; 1 x 200000 6.1 / 12.6, 12.6 / 21.7, 16.4 / 24.6; 64 x 100000 8.2 / 8.4, 18.0 / 15.3, 22.3 / 18.2; 64 x 200000 10.0 / 13.1,
+// 20.2 / 22.3, 26.4 / 28.5; 200 x 200000 17.3 / 15.5, 29.3 / 21.6, 49.5 / 33.9.  The threshold is one for all: 32 to 64 rows with alternatives
+// lose up to 22 % by it as far as some 150,000 classes of 16 bits or fp32.
 static LogProbsPlan plan_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, adapt_fmt f)
 {
     const int U = f.wl != ADAPT_WL_FP32 && f.wl <= 8 ? 16 : 8;
@@ -891,8 +893,11 @@ size_t ws_need_log_probs(int num_cu, uint64_t rows, uint64_t classes, int topk, 
 }
 
 // How the rows of a cross entropy are cut.  Chunks of a row, whose sums are a launch of their own, for few and long rows: us in a captured
-// graph, chunks / a block per row: 1 x 28723 of 8 bits (1795 units) 8.7 / 7.4, 16 bits (3590) 9.1 / 10.7, fp32 10.8 / 16.3; 64 x 28723
-// 10.1 / 8.0, 11.4 / 11.9, 13.6 / 17.4; 100 x 100000 14.6 / 15.6, 22 / 33, 31 / 54; 200 x 100000 19.9 / 16.9, 32.3 / 30.9, 47.1 / 46.9.
+// graph, chunks / a block per row, 8 bits, 16 bits, fp32: one row of 2500 units 8.3 / 7.8, 8.9 / 8.4, 10.1 / 12.2, of 3200 8.5 / 8.9, 8.7 / 9.7,
+// 9.9 / 14.3, of 5000 8.2 / 11.7, 8.6 / 12.8, 9.8 / 19.1; 64 rows of 2500 units 9.9 / 8.6, 10.6 / 9.2, 12.3 / 12.9, of 3200 10.2 / 9.9, 10.8 / 10.4,
+// 12.5 / 15.2, of 5000 10.5 / 12.9, 11.4 / 13.9, 12.6 / 20.0; 128 rows of 3200 units 11.4 / 10.2, 12.5 / 11.1, 14.3 / 15.3, of 5000 13.3 / 13.4,
+// 14.6 / 14.8, 17.4 / 20.3; 200 x 100000 classes 19.9 / 16.9, 32.3 / 30.9, 47.1 / 46.9.  The threshold is where 8 and 16 bits meet at up to 64 rows;
+// 65 to 128 rows of them lose up to 16 % between it and 5000 units, and one row of fp32 would gain from 1800 on.
 // Threads: one unit each where every row has a compute unit of its own (1 x 5000, 1, 2, 4 units: 4.4, 5.0, 5.5), two where blocks are few
 // (400 x 5000 of 16 bits, 1, 2, 4: 8.2, 7.5, 8.4), otherwise eight and at most 512 threads: 256, 512, 1024 threads take 8192 x 32000 of
 // 8 bits 140, 151, 190; 1536 x 65531 of 16 bits 186, 157, 163; 1024 x 50001 fp32 129, 125, 126.
@@ -1018,7 +1023,8 @@ static FixedReference fixed_reference(int wl, int fl)
 template <typename T, typename G>
 static void launch_cross_entropy(adapt_ctx *ctx, const LogitArgs &a, const CrossEntropyPlan &p, int wl)
 {
-    // Codes of 96 MiB or more leave the caches before the next call reads them, and take the room that the sweeps need.  us, in the
+    // Codes of 8 and 16 bits that take 96 MiB or more leave the caches before the next call reads them, and take the room that the sweeps
+    // need (wider ones always go through them: not measured past them).  us, in the
     // caches / past them, alone and with a copy of the codes behind: 62 MiB (2048 x 32000, 8 bits) 33.5 / 33.4, 51 / 57; 125 MiB (4096)
     // 74 / 60, 127 / 123; 128 MiB (1024 x 65531, 16 bits) 83 / 66, 133 / 126; 250 MiB (8192 x 32000, 8 bits) 134 / 127, 231 / 229
     const bool past = a.rows * a.classes * sizeof(G) >= ((uint64_t)96 << 20);
